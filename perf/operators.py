@@ -155,7 +155,7 @@ def _product_key(g):
 
 
 def _round(v):
-    return int(math.floor(abs(v) + 0.5)) * (1 if v >= 0 else -1)
+    return int(v) if abs(v) >= 2.0 ** 52 else int(math.floor(abs(v) + 0.5)) * (1 if v >= 0 else -1)
 
 
 def _layout(case):
