@@ -167,19 +167,16 @@ def _layout(case):
 
 
 def _sums(case):
-    """The sums of rotations that leave the sum over a plane in each of its slots: a copy one block to the right, then
-    doublings, up to three of them as one sum."""
+    """The sums of rotations that leave the sum over a ciphertext's elements in every slot that is a multiple of the strides'
+    common power of two away from one: doublings up to all slots, up to three of them as one sum."""
     h, w, hs, ws, c, cs = _layout(case)
-    slots = 1 << (case["log_n"] - 1)
-    span = (h - 1) * hs + (w - 1) * ws + (c - 1) * cs + 1
-    block = 1 << (span - 1).bit_length()
-    unit = block
+    slots = unit = 1 << (case["log_n"] - 1)
     for count, stride in ((h, hs), (w, ws), (c, cs)):
         while count > 1 and stride % unit:
             unit //= 2
-    amounts = [[slots - block]] if block < slots and block > unit else []
-    while unit < block:
-        few = min(3, (block // unit).bit_length() - 1)
+    amounts = []
+    while unit < slots:
+        few = min(3, (slots // unit).bit_length() - 1)
         amounts.append([k * unit for k in range(1, 1 << few)])
         unit <<= few
     return amounts
