@@ -154,6 +154,11 @@ def _product_key(g):
     return (1 << 32) | g        # the key from s * sigma_g(s): the identifier that hisa_gen_rot_mul_keys gives it
 
 
+def _scale(case):
+    """What a program encrypts at: the size of the primes, so that a product rescaled is at that scale again."""
+    return 2.0 ** case["bits"]
+
+
 def _round(v):
     return int(v) if abs(v) >= 2.0 ** 52 else int(math.floor(abs(v) + 0.5)) * (1 if v >= 0 else -1)
 
@@ -209,8 +214,7 @@ def _cubic(a, b):
     return c3 * s, c3, c3 * low, 2.0 - c3 * low
 
 
-SCALE = 2.0 ** 40
-NORM = {"eps": 1e-3, "lo": 0.05, "hi": 2.0, "ratio": 0.5}
+NORM = {"eps": 1e-3, "lo": 0.05, "hi": 2.0, "ratio": 0.5, "share": 1.0 / 64.0}
 
 
 # --- the plain form: residues as int64 arrays [..., limbs, N] ---
@@ -359,21 +363,21 @@ def _rotated_products(ring, keys, a, b, g, shared, add=None, factor=0, summed=Fa
     return _switch(ring, torch.stack(e[:2], 1), e[2:], [keys[g], keys[_product_key(g)]], level)
 
 
-def _products(ring, keys, a, b, add=None, factor=0, negative=False, shared=1):
-    """(+-)a b (+ factor add), relinearised and rescaled."""
+def _products(ring, keys, a, b, add=None, factor=0, factor_ab=1, shared=1):
+    """factor_ab a b (+ factor add), relinearised and rescaled."""
     level = min(a.shape[-2], b.shape[-2])
     p = ring.column(ring.ids(level))
     a, b = a[:, :, :level].repeat_interleave(shared, 0), b[:, :, :level]
     e = [_mul(a[:, 0], b[:, 0], p), torch.remainder(_mul(a[:, 0], b[:, 1], p) + _mul(a[:, 1], b[:, 0], p), p), _mul(a[:, 1], b[:, 1], p)]
-    if negative:
-        e = [torch.remainder(-v, p) for v in e]
+    if factor_ab != 1:
+        e = [_times(ring, v, factor_ab, level) for v in e]
     if add is not None:
         e[:2] = [torch.remainder(e[i] + _times(ring, add[:, i, :level], factor, level), p) for i in (0, 1)]
     return _switch(ring, torch.stack(e[:2], 1), e[2:], [keys[0]], level)
 
 
 def _plain_scan(ring, keys, case, gates, x, reverse):
-    scale, shared = SCALE, case["shared"]
+    scale, shared = _scale(case), case["shared"]
     steps = _scan_steps(case, reverse)
     for i, step in enumerate(steps):
         g, last = _galois(case, step), ring.primes[min(gates.shape[-2], x.shape[-2]) - 1]
@@ -393,6 +397,7 @@ def _rotate(ring, keys, case, x, step):
 
 def _plain_norm(state):
     ring, keys, case, x = state["ring"], state["keys"], state["case"], state["x"]
+    scale = _scale(case)
     level, per = x.shape[-2], x.shape[0] // (case["batch"] * case["groups"])
     p = ring.column(ring.ids(level))
     n = case["channels"] // case["groups"] * case["side"] * case["side"]
@@ -413,27 +418,29 @@ def _plain_norm(state):
         acc = _with_p(ring, torch.remainder(acc, ring.column(ring.ids(level, True))), plain, level)
         both = _divide(ring, acc, level, _specials(ring))
     first, second = both.chunk(2)
-    # n^2 times the variance, then its share of the largest one at the inputs' scale, with eps
-    variance = _products(ring, keys, first, first, second, n, negative=True)
-    s = SCALE * SCALE / q(level) * n * n * NORM["hi"]
+    # n^2 times the variance; its share of the largest one, with eps, once for the iterations and once for the line they start from
+    variance = _products(ring, keys, first, first, second, n, factor_ab=-1)
+    s = scale * scale / q(level) * n * n * NORM["hi"]
     level -= 1
-    k = _round(SCALE * q(level) / s)
-    w = _divide(ring, _times(ring, variance, k, level), level, [level - 1])
-    s_w = s * k / q(level)
+    c1, c3, a, b = _cubic(math.sqrt(NORM["lo"] / NORM["hi"]), 1.0)
+    k_w, k_y = (max(1, _round(scale * share * q(level) / s)) for share in (NORM["share"], c3))
+    w, y = (_divide(ring, _times(ring, variance, k, level), level, [level - 1]) for k in (k_w, k_y))
+    s_w, s_y = s * k_w / q(level), s * k_y / q(level) / c3
     level -= 1
     w[:, 0] = _shifted(ring, w[:, 0], _round(NORM["eps"] / NORM["hi"] * s_w), level)
     # 1 / sqrt by odd cubics
-    c1, c3, a, b = _cubic(math.sqrt(NORM["lo"] / NORM["hi"]), 1.0)
-    s_y = s_w / c3
-    y = torch.remainder(-w, ring.column(ring.ids(level)))
-    y[:, 0] = _shifted(ring, y[:, 0], _round(c1 * s_y), level)
+    y = torch.remainder(-y, ring.column(ring.ids(level)))
+    y[:, 0] = _shifted(ring, y[:, 0], _round((c1 - c3 * (NORM["eps"] / NORM["hi"])) * s_y), level)
     for _ in range(case["iterations"]):
         c1, c3, a, b = _cubic(a, b)
         s_1, s_2 = s_w * s_y / q(level) / c3, s_y * s_y / q(level)
         one, two = _products(ring, keys, w, y), _products(ring, keys, y, y)
         level -= 1
-        y = _products(ring, keys, one, two, y, _round(c1 * s_1 * s_2 / s_y), negative=True)
-        s_y = s_1 * s_2 / q(level)
+        s_3 = s_1 * s_2
+        m = max(1, _round(scale * q(level) / s_3))
+        s_3 *= m
+        y = _products(ring, keys, one, two, y, _round(c1 * s_3 / s_y), factor_ab=-m)
+        s_y = s_3 / q(level)
         level -= 1
     s_y *= math.sqrt(NORM["hi"])
     # (x - mean) gamma, times it, plus beta
@@ -444,7 +451,7 @@ def _plain_norm(state):
     images = x.shape[0] // gamma.shape[0]
     centred = _mul(centred, gamma.repeat(images, 1, 1)[:, None], p)
     centred = _divide(ring, centred, level + 1, [level])
-    s_out = SCALE * n * state["gamma_scale"] / q(level + 1) * s_y / q(level)
+    s_out = scale * n * state["gamma_scale"] / q(level + 1) * s_y / q(level)
     out = _products(ring, keys, y, centred, shared=per)
     level -= 1
     out[:, 0] = torch.remainder(out[:, 0] + beta.repeat(images, 1, 1), ring.column(ring.ids(level)))
@@ -498,7 +505,7 @@ class _Program:
 
     def tensor(self, case, residues, channels):
         batch = case.get("batch", 1)
-        cts = self.ctx.ct_random_batch(residues.shape[0], residues.shape[2], SCALE, 1)
+        cts = self.ctx.ct_random_batch(residues.shape[0], residues.shape[2], _scale(case), 1)
         self.view(cts).copy_(residues)
         torch.cuda.synchronize()
         h, w, hs, ws, c, cs = _layout(case)
@@ -534,7 +541,8 @@ def _inputs(case, seed, primes):
     if case["op"] == "norm":
         per_image = case["channels"] // case["c_inner"]
         small = lambda k, bits: _uniform(1000003 * k, per_image, [1 << bits], n)[:, 0] - (1 << (bits - 1))  # noqa: E731
-        return {"x": make(0, case["batch"] * per_image), "gamma": small(1, 30), "gamma_scale": 2.0 ** 27, "beta": small(2, 40)}
+        n_el = case["channels"] // case["groups"] * case["side"] ** 2
+        return {"x": make(0, case["batch"] * per_image), "gamma": small(1, 30), "gamma_scale": _scale(case) / n_el, "beta": small(2, 40)}
     gates = case["cts"] // case["shared"]
     state = {"gates": make(0, gates), "x": make(1, case["cts"])}
     if case["op"] != "scan":
@@ -580,7 +588,7 @@ def run(state):
         return _plain_norm(state)
     ring, keys, gates, x = state["ring"], state["keys"], state["gates"], state["x"]
     if op == "step":
-        return _products(ring, keys, gates, state["state"], x, _round(SCALE * SCALE / SCALE), shared=case["shared"])
+        return _products(ring, keys, gates, state["state"], x, _round(_scale(case)), shared=case["shared"])
     if op == "scan":
         return _plain_scan(ring, keys, case, gates, x, case["reverse"])
     # grad: x is the gradient of h, state is h; the gates move one token, the scan runs the other way
@@ -791,10 +799,10 @@ def exact(case, seed):
         return finish(_exact_norm(X, case, keys, data))
     shared, gates = case["shared"], list(data["gates"])
     if case["op"] == "step":
-        return finish([X.product(keys, gates[i // shared], data["state"][i], 1, data["x"][i], _round(SCALE)) for i in range(case["cts"])])
+        return finish([X.product(keys, gates[i // shared], data["state"][i], 1, data["x"][i], _round(_scale(case))) for i in range(case["cts"])])
 
     def scan(gates, x, reverse):
-        scale = SCALE
+        scale = _scale(case)
         for i in range(len(_scan_steps(case, reverse))):
             g = _galois(case, _scan_steps(case, reverse)[i])
             last = X.primes[min(gates[0].shape[1], x[0].shape[1]) - 1]
@@ -813,7 +821,7 @@ def exact(case, seed):
 
 
 def _exact_norm(X, case, keys, data):
-    x, level = list(data["x"]), case["level"]
+    x, level, scale = list(data["x"]), case["level"], _scale(case)
     per, q = len(x) // (case["batch"] * case["groups"]), lambda l: X.primes[l - 1]
     n = case["channels"] // case["groups"] * case["side"] ** 2
     h, out = NORM, []
@@ -830,23 +838,23 @@ def _exact_norm(X, case, keys, data):
             m, sq = (X.switch([sum((X.rotated(v[0], g) for g in gs), v[0]) % np.array(X.primes[:l])[:, None], v[1]], [v[1]],
                               [[(keys(g), g) for g in gs]], l, X.special()) for v in (m, sq))
         v = X.product(keys, m, m, -1, sq, n)
-        s = SCALE * SCALE / q(l) * n * n * h["hi"]
-        k = _round(SCALE * q(l - 1) / s)
-        w = np.stack([X.divide(X.scaled(v[u], k), list(range(l - 1)), [l - 2]) for u in (0, 1)])
-        s_w, l = s * k / q(l - 1), l - 2
+        s = scale * scale / q(l) * n * n * h["hi"]
+        c1, c3, a, b = _cubic(math.sqrt(h["lo"] / h["hi"]), 1.0)
+        k_w, k_y = (max(1, _round(scale * share * q(l - 1) / s)) for share in (h["share"], c3))
+        w, y = (np.stack([X.divide(X.scaled(v[u], k), list(range(l - 1)), [l - 2]) for u in (0, 1)]) for k in (k_w, -k_y))
+        s_w, s_y, l = s * k_w / q(l - 1), s * k_y / q(l - 1) / c3, l - 2
         const = lambda c: np.full((l, X.n), 1, dtype=np.int64) * np.array([c % p for p in X.primes[:l]])[:, None]  # noqa: E731
         w[0] = X.add(w[0], const(_round(h["eps"] / h["hi"] * s_w)))
-        c1, c3, a, b = _cubic(math.sqrt(h["lo"] / h["hi"]), 1.0)
-        s_y = s_w / c3
-        y = np.stack([X.scaled(w[0], -1), X.scaled(w[1], -1)])
-        y[0] = X.add(y[0], const(_round(c1 * s_y)))
+        y[0] = X.add(y[0], const(_round((c1 - c3 * (h["eps"] / h["hi"])) * s_y)))
         for _ in range(case["iterations"]):
             c1, c3, a, b = _cubic(a, b)
-            s_1, s_2 = s_w * s_y / q(l) / c3, s_y * s_y / q(l)
-            y = X.product(keys, X.product(keys, w, y), X.product(keys, y, y), -1, y, _round(c1 * s_1 * s_2 / s_y))
-            s_y, l = s_1 * s_2 / q(l - 1), l - 2
+            s_3 = s_w * s_y / q(l) / c3 * (s_y * s_y / q(l))
+            up = max(1, _round(scale * q(l - 1) / s_3))
+            s_3 *= up
+            y = X.product(keys, X.product(keys, w, y), X.product(keys, y, y), -up, y, _round(c1 * s_3 / s_y))
+            s_y, l = s_3 / q(l - 1), l - 2
         s_y *= math.sqrt(h["hi"])
-        s_out = SCALE * n * data["gamma_scale"] / q(l + 1) * s_y / q(l)
+        s_out = scale * n * data["gamma_scale"] / q(l + 1) * s_y / q(l)
         for i, c in enumerate(group):
             place = (at + i) % data["gamma"].shape[0]
             plain = lambda t, limbs: np.stack([X.values(data[t][place].cpu().numpy() % X.primes[j], j) for j in range(limbs)])  # noqa: E731
