@@ -96,6 +96,10 @@ int hisa_sync(hisa_ctx* ctx);
  * modulo N/2, zero and repeats are skipped. */
 int hisa_keygen(hisa_ctx* ctx);
 int hisa_gen_rot_keys(hisa_ctx* ctx, const int32_t* left_steps, size_t n);
+/* For products of rotated ciphertexts (the recurrence below): the same amounts' rotation keys, and beside each the key from
+ * s * sigma(s), with which a rot(b) is relinearised and rotated by one division.  Needs what hisa_rot_left_sum_batch
+ * needs (HISA_ERR_ARG otherwise). */
+int hisa_gen_rot_mul_keys(hisa_ctx* ctx, const int32_t* left_steps, size_t n);
 
 /* ---- Integers profile: encode / decode (Fig. "Instructions of the HISA") ----
  * The HEAAN family packs N/2 complex numbers (Sec. "HEAAN"); host arrays
@@ -540,6 +544,72 @@ int hisa_avg_pool2x2(hisa_ctx* ctx, const hisa_tensor* in, hisa_tensor* out);
  * relinearisation, one mulScalar by b/a at scale = ciphertext scale, one add,
  * one divScalar.  The factor a belongs in the next layer's weights. */
 int hisa_poly2_act(hisa_ctx* ctx, const hisa_tensor* in, double a, double b, hisa_tensor* out);
+/* ---- layers of sequence models (no counterpart in the paper; its interface is what they are made of) ----
+ * They need what hisa_rot_left_sum_batch needs (HISA_ERR_ARG otherwise), clean tensors, and one scale per tensor
+ * (HISA_ERR_SCALE_MISMATCH).  Operands may differ in level: each is used at the lowest one among them.
+ *
+ * Gated linear recurrence along the width of a tensor, every row (batch, channel, y) a sequence of its own:
+ *     h[t] = x[t] + gates[t] h[t - 1],  h[first] = x[first];  reverse != 0: h[t] = x[t] + gates[t] h[t + 1]
+ * Gates have the layout of x; x may have m times as many channels, gate ciphertext g then serves ciphertexts g m .. g m + m - 1
+ * of each image (heads that share a gate; HISA_ERR_ARG where the channels do not divide so).  The gates of the first
+ * token of every row (reverse: of the last) have to be encryptions of zero -- they multiply nothing, and the zero keeps the
+ * rows of a ciphertext apart: hisa_recurrence_gates makes it so by one masking multiply (one level; _fixed with the mask as
+ * mask_coeffs[ceil(C/c_inner)][N] at mask_scale).  A scan over T = width tokens takes ceil(log2 T) levels
+ * (HISA_ERR_DEPTH_EXHAUSTED), each a product of rotated ciphertexts a rot(b) with the two key switches it takes and the
+ * rescale as one division; T = 1 gives x.  Output: x's layout, clean, scale of the gates times that of x over the last
+ * modulus per level.
+ * hisa_recurrence_step is one token: out = x + gates * state element by element (any width; one level, the relinearisation
+ * key).  x is taken times a whole number to the scale of gates times that of state (HISA_ERR_SCALE_MISMATCH where none is
+ * within 2^-16 of what that takes, here and in the other layers: scales have to be about as large as the primes).  With a state whose elements are zero but at the first token, it puts a state in front of a scan: the scan
+ * of the result with the masked gates continues the sequence that ended in that state.
+ * hisa_recurrence_grad is the backward pass: from the gates (masked, as above), the states h that the scan returned and the
+ * gradient of those, dx = gradient of x and dgates = gradient of the gates, summed over the channels that share them (T >= 2):
+ * ceil(log2 T) levels for dx and one more for dgates.  dgates is not clean and holds nothing meaningful at the first token
+ * (reverse: the last), whose gate is a constant: hisa_recurrence_gates of it is the gradient of gates before their mask.
+ * hisa_recurrence_rot_steps lists the amounts for hisa_gen_rot_mul_keys; backward != 0: those of hisa_recurrence_grad. */
+int hisa_recurrence(hisa_ctx* ctx, const hisa_tensor* gates, const hisa_tensor* x, uint32_t reverse, hisa_tensor* out);
+int hisa_recurrence_step(hisa_ctx* ctx, const hisa_tensor* gates, const hisa_tensor* state, const hisa_tensor* x,
+                         hisa_tensor* out);
+int hisa_recurrence_grad(hisa_ctx* ctx, const hisa_tensor* gates, const hisa_tensor* h, const hisa_tensor* grad,
+                         uint32_t reverse, hisa_tensor* dx, hisa_tensor* dgates);
+int hisa_recurrence_gates(hisa_ctx* ctx, const hisa_tensor* gates, uint32_t reverse, hisa_tensor* out);
+int hisa_recurrence_gates_fixed(hisa_ctx* ctx, const hisa_tensor* gates, const int64_t* mask_coeffs, double mask_scale,
+                                hisa_tensor* out);
+int hisa_recurrence_rot_steps(hisa_ctx* ctx, const hisa_tensor* like, uint32_t reverse, uint32_t backward, int32_t* steps,
+                              size_t cap, size_t* n);
+/* Group normalisation over the elements of channels / groups neighbouring channels of an image, n of them, with an optional
+ * degree-2 activation behind it:
+ *     y = gamma[c] (x - mean) / sqrt(var + eps) + beta[c],   var = mean of (x - mean)^2;   act = 1: y^2 + act_ratio y
+ * (a y^2 + b y is a times the latter with act_ratio = b / a; the factor belongs in the next layer's weights, as with
+ * hisa_poly2_act).  HW- and CHW-tiled tensors, channels last among them (c_stride = 1, w_stride = c_inner); a ciphertext
+ * may hold channels of one group only (HISA_ERR_ARG).  groups = 1 is a layer norm of the whole image, groups = channels an
+ * instance norm.
+ * 1 / sqrt is a line and `iterations` odd cubics, y <- c1 y - c3 v y^3, each the one that stays nearest to its target on
+ * what the step before leaves of [var_lo, var_hi]: var + eps has to lie in there (above it the result is nothing, below it
+ * falls short).  The largest relative error of 1 / sqrt for var_hi / var_lo = 16 is 7e-2, 4e-3, 1e-5, 7e-11 with 1, 2, 3, 4
+ * iterations, for 100 0.31, 7e-2, 4e-3, 1e-5.  var is n sum x^2 - (sum x)^2, so means far beyond the deviations cost
+ * precision.  Levels: 3 + 2 iterations, one more with the activation.  Needs the relinearisation key and the rotation keys
+ * that hisa_group_norm_rot_steps lists.
+ * hisa_group_norm_prepare encodes gamma and beta (host, [channels]; null: one, zero) for tensors with the layout, level and
+ * scale of `like` into a plan that owns device memory until hisa_group_norm_plan_free; _prepare_fixed takes coefficients
+ * [ceil(C/c_inner)][N], gamma's at gamma_scale, beta's at the scale of the normalised values.  Prepared like this gamma is at
+ * 1 / n of a modulus, and outputs are near the scale of the inputs.  hisa_group_norm_apply: another layout is HISA_ERR_ARG,
+ * another level HISA_ERR_LEVEL_MISMATCH, another scale HISA_ERR_SCALE_MISMATCH.  Output: the input's layout, clean. */
+typedef struct {
+    uint32_t groups, iterations;  /* iterations 1 .. 16 */
+    double eps, var_lo, var_hi;   /* 0 <= eps <= var_hi, 0 < var_lo < var_hi */
+    double act_ratio;
+    uint32_t act;                 /* 0 or 1 */
+    uint32_t reserved;
+} hisa_norm_geom;
+typedef struct hisa_norm_plan hisa_norm_plan;
+int hisa_group_norm_prepare(hisa_ctx* ctx, const hisa_tensor* like, const double* gamma, const double* beta,
+                            const hisa_norm_geom* geom, hisa_norm_plan** plan);
+int hisa_group_norm_prepare_fixed(hisa_ctx* ctx, const hisa_tensor* like, const int64_t* gamma_coeffs, double gamma_scale,
+                                  const int64_t* beta_coeffs, const hisa_norm_geom* geom, hisa_norm_plan** plan);
+int hisa_group_norm_apply(hisa_ctx* ctx, const hisa_tensor* in, const hisa_norm_plan* plan, hisa_tensor* out);
+int hisa_group_norm_plan_free(hisa_ctx* ctx, hisa_norm_plan* plan);
+int hisa_group_norm_rot_steps(hisa_ctx* ctx, const hisa_tensor* in, int32_t* steps, size_t cap, size_t* n);
 /* The left-rotation amounts a layer will use on this input layout, for
  * hisa_gen_rot_keys (the rotation-key selection of Sec. "Rotation Keys
  * Selection"): writes at most cap amounts to host steps[], the count to *n.
@@ -564,7 +634,9 @@ int hisa_tensor_free(hisa_ctx* ctx, hisa_tensor* t);
  * consecutive device polynomials dev_buf[n_polys][N] modulo prime prime_index
  * (0..L-1: q_i, L..L+alpha-1: special); forward output index i holds
  * a(psi^(2*bitrev(i)+1)).  key_export: host[dnum][2][L+alpha][N], NTT form,
- * (b, a) per digit; key_id 0 = relinearisation key, else a Galois element. */
+ * (b, a) per digit; key_id 0 = relinearisation key, else a Galois element g of a rotation, 2^32 + g the key from
+ * s * sigma_g(s).  key_import: the inverse, for a server that is sent its evaluation keys (residues are checked,
+ * HISA_ERR_ARG; a key that is there is replaced). */
 int hisa_get_primes(hisa_ctx* ctx, uint64_t* q, uint64_t* p);
 int hisa_get_alpha(hisa_ctx* ctx, uint32_t* alpha);
 int hisa_ct_info(const hisa_ct* ct, uint32_t* limbs, uint32_t* polys, double* scale);
@@ -575,6 +647,7 @@ int hisa_ct_import_batch(hisa_ctx* ctx, const uint64_t* host, size_t n, uint32_t
 int hisa_ct_device_ptr(const hisa_ct* ct, uint64_t** dev);
 int hisa_ntt_raw(hisa_ctx* ctx, uint64_t* dev_buf, uint32_t prime_index, size_t n_polys, int inverse);
 int hisa_key_export(hisa_ctx* ctx, uint64_t key_id, uint64_t* host);
+int hisa_key_import(hisa_ctx* ctx, uint64_t key_id, const uint64_t* host);
 int hisa_galois_elt(hisa_ctx* ctx, int32_t left_steps, uint64_t* g);
 int hisa_secret_export(hisa_ctx* ctx, int64_t* host_coeffs);
 

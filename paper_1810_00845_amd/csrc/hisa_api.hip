@@ -765,7 +765,7 @@ extern "C" int hisa_keygen(hisa_ctx* ctx) {
     return gen_switch_key(ctx, 0, s2.u());
 }
 
-static u64 galois_of(const hisa_ctx* ctx, int32_t steps) {
+u64 galois_of(const hisa_ctx* ctx, int32_t steps) {
     const u64 slots = ctx->N / 2, mask = 2 * (u64)ctx->N - 1;
     i64 r = (i64)steps % (i64)slots;
     if (r < 0) r += (i64)slots;
@@ -791,6 +791,22 @@ extern "C" int hisa_gen_rot_keys(hisa_ctx* ctx, const int32_t* left_steps, size_
         if (!tgt.ok()) return HISA_ERR_OOM;
         HIP_TRY(ctx, launch_automorph_ntt(ctx->d_secret, 0, tgt.u(), 0, g, (int)ctx->total, 1, (int)ctx->log_n, ctx->stream));
         TRY(gen_switch_key(ctx, g, tgt.u()));
+    }
+    return HISA_OK;
+}
+
+extern "C" int hisa_gen_rot_mul_keys(hisa_ctx* ctx, const int32_t* left_steps, size_t count) {
+    if (!ctx) return HISA_ERR_ARG;
+    if (!fused_key_switch_available(ctx)) return fail(ctx, HISA_ERR_ARG, "products of rotated ciphertexts need " FUSED_PATH);
+    TRY(hisa_gen_rot_keys(ctx, left_steps, count));
+    for (size_t i = 0; i < count; i++) {
+        const u64 g = galois_of(ctx, left_steps[i]);
+        if (g == 0 || ctx->keys.count(product_key_id(g))) continue;
+        Temp tgt(ctx, (size_t)ctx->total * ctx->N * sizeof(u64));
+        if (!tgt.ok()) return HISA_ERR_OOM;
+        HIP_TRY(ctx, launch_automorph_ntt(ctx->d_secret, 0, tgt.u(), 0, g, (int)ctx->total, 1, (int)ctx->log_n, ctx->stream));
+        HIP_TRY(ctx, launch_pointwise_mul(ctx->d_primes, ctx->d_secret, tgt.u(), tgt.u(), (int)ctx->total, (int)ctx->log_n, ctx->stream));
+        TRY(gen_switch_key(ctx, product_key_id(g), tgt.u()));
     }
     return HISA_OK;
 }
@@ -1864,6 +1880,58 @@ int relinearize_rescale_fp(hisa_ctx* ctx, const u64* cts3, u64 stride, size_t n_
     return key_switch_core_fp(ctx, cts3 + 2 * lw, stride, 0, n_cts, l, it->second, cts3, stride, 2, by, out);
 }
 
+int relinearize_fp(hisa_ctx* ctx, const u64* cts3, size_t n, int l, u64* out) {
+    if (!fused_key_switch_available(ctx)) return fail(ctx, HISA_ERR_ARG, "no fused key-switch path for these parameters");
+    if (t_analysis) {
+        TALLY(relinearize, HISA_OP_RELINEARIZE, n, l);
+        TALLY(key_switch_calls, HISA_OP_KEY_SWITCH_CALLS, 1, l);
+        return HISA_OK;
+    }
+    auto it = ctx->keys.find(0);
+    if (it == ctx->keys.end()) return fail(ctx, HISA_ERR_NO_KEY, "no relinearisation key: call hisa_keygen");
+    const size_t lw = (size_t)l * ctx->N;
+    Division by;
+    TRY(division_by_p(ctx, l, false, &by));
+    return key_switch_core_fp(ctx, cts3 + 2 * lw, 3 * lw, 0, n, l, it->second, cts3, 3 * lw, 2, by, out);
+}
+
+int product_keys_present(hisa_ctx* ctx, int32_t steps) {
+    const u64 g = galois_of(ctx, steps);
+    if (g == 0) return fail(ctx, HISA_ERR_ARG, "rotation by a multiple of the slot count");
+    if (t_analysis) {
+        t_analysis->steps.insert(norm_step(ctx, steps));
+        return HISA_OK;
+    }
+    if (ctx->keys.find(g) == ctx->keys.end() || ctx->keys.find(product_key_id(g)) == ctx->keys.end())
+        return fail(ctx, HISA_ERR_NO_KEY, "no keys for products rotated by %d slots: call hisa_gen_rot_mul_keys", steps);
+    return HISA_OK;
+}
+
+int rotated_products_fp(hisa_ctx* ctx, const u64* pairs, const u64* plain, size_t n_pairs, int l, int32_t steps, u64* out) {
+    if (!fused_key_switch_available(ctx)) return fail(ctx, HISA_ERR_ARG, "no fused key-switch path for these parameters");
+    TRY(product_keys_present(ctx, steps));
+    if (l < 2) return fail(ctx, HISA_ERR_DEPTH_EXHAUSTED, "no level to rescale into");
+    if (t_analysis) {
+        TALLY(rot_left, HISA_OP_ROT_LEFT, n_pairs, l);
+        TALLY(mul, HISA_OP_MUL, n_pairs, l);
+        TALLY(relinearize, HISA_OP_RELINEARIZE, n_pairs, l);
+        TALLY(rescale, HISA_OP_RESCALE, n_pairs, l);
+        TALLY(key_switch_calls, HISA_OP_KEY_SWITCH_CALLS, 1, l);
+        return HISA_OK;
+    }
+    const u64 g = galois_of(ctx, steps);
+    const SwitchKey &key = ctx->keys.find(g)->second, &key2 = ctx->keys.find(product_key_id(g))->second;
+    const size_t n = ctx->N;
+    const int K = (int)ctx->K, ext_limbs = l + K;
+    FpExt x(ctx, 2 * n_pairs, l, K, (int)ctx->alpha);
+    Temp acc(ctx, n_pairs * 2 * (size_t)ext_limbs * n * sizeof(u64));
+    if (!x.ok() || !acc.ok()) return HISA_ERR_OOM;
+    TRY(key_switch_modup_fp(ctx, pairs, (u64)l * n, 2 * n_pairs, x));
+    HIP_TRY(ctx, launch_pair_inner_fp(ctx->tabs.fprimes, x.extp, x.digits, l, K, (int)ctx->L, (int)ctx->alpha, key.data, key2.data,
+                                      (int)ctx->total, pairs, plain, ctx->d_pmod, acc.u(), n_pairs, (int)ctx->log_n, ctx->stream));
+    return moddown_rescale_fp(ctx, acc.u(), n_pairs, l, nullptr, 0, 0, out);
+}
+
 static int key_switch_core(hisa_ctx* ctx, const u64* d, u64 d_bs, u64 galois, size_t B, int l, const SwitchKey& key, const u64* add,
                            u64 add_bs, int add_polys, u64* out) {
     if (!fused_key_switch_available(ctx)) return key_switch_core_int(ctx, d, d_bs, galois, B, l, key, add, add_bs, add_polys, out);
@@ -2196,6 +2264,12 @@ static int rescale_core_fp(hisa_ctx* ctx, const u64* in, size_t n_bp, int l, u64
     return divide_fp(ctx, c);
 }
 
+int rescale_fp(hisa_ctx* ctx, const u64* in, size_t n_polys, int l, u64* out) {
+    if (l < 2) return fail(ctx, HISA_ERR_DEPTH_EXHAUSTED, "no level to rescale into");
+    if (t_analysis) TALLY(rescale, HISA_OP_RESCALE, (n_polys + 1) / 2, l);
+    return rescale_core_fp(ctx, in, n_polys, l, out);
+}
+
 // the same in integers
 static int rescale_core_int(hisa_ctx* ctx, const u64* in, size_t n_bp, int l, u64* out) {
     const size_t nn = ctx->N, chunk = std::min<size_t>(n_bp, 65535);
@@ -2347,6 +2421,37 @@ extern "C" int hisa_key_export(hisa_ctx* ctx, uint64_t key_id, uint64_t* host) {
     }
     HIP_TRY(ctx, hipMemcpyAsync(host, it->second.data, words * sizeof(u64), hipMemcpyDeviceToHost, ctx->stream));
     HIP_TRY(ctx, hipStreamSynchronize(ctx->stream));
+    return HISA_OK;
+}
+
+extern "C" int hisa_key_import(hisa_ctx* ctx, uint64_t key_id, const uint64_t* host) {
+    if (!ctx || !host) return fail(ctx, HISA_ERR_ARG, "bad argument");
+    if (t_analysis) return fail(ctx, HISA_ERR_ARG, "keys cannot be imported during an analysis (no kernel runs)");
+    const u64 g = key_id & 0xffffffffu, kind = key_id >> 32;
+    const bool galois = (g & 1) && g > 1 && g < 2 * (u64)ctx->N;
+    if (!(key_id == 0 || (kind <= 1 && galois))) return fail(ctx, HISA_ERR_ARG, "%llu names no key", (unsigned long long)key_id);
+    const size_t n = ctx->N, rows = (size_t)ctx->dnum * 2 * ctx->total, words = rows * n;
+    for (size_t r = 0; r < rows; r++)
+        for (size_t j = 0; j < n; j++)
+            if (host[r * n + j] >= ctx->mod[r % ctx->total]) return fail(ctx, HISA_ERR_ARG, "a value of the key is no residue of its prime");
+    auto it = ctx->keys.find(key_id);
+    u64* data = it == ctx->keys.end() ? nullptr : it->second.data;
+    if (!data) {
+        void* p = nullptr;
+        HIP_TRY(ctx, hipMalloc(&p, words * sizeof(u64)));
+        data = (u64*)p;
+    }
+    hipError_t e = hipMemcpyAsync(data, host, words * sizeof(u64), hipMemcpyHostToDevice, ctx->stream);
+    if (e == hipSuccess && fused_key_switch_available(ctx))
+        e = launch_key_to_doubles(ctx->d_fprimes, data, (int)ctx->dnum * 2, (int)ctx->total, (int)ctx->log_n, ctx->stream);
+    const hipError_t waited = hipStreamSynchronize(ctx->stream);       // the caller's array may go
+    if (e == hipSuccess) e = waited;
+    if (e != hipSuccess) {       // nothing half written is left behind
+        if (it != ctx->keys.end()) { delete it->second.blk; ctx->keys.erase(it); }
+        (void)hipFree(data);
+        return fail(ctx, HISA_ERR_HIP, "key import: %s", hipGetErrorString(e));
+    }
+    if (it == ctx->keys.end()) ctx->keys[key_id] = SwitchKey{new DevBlock{data, words * sizeof(u64), 1}, data};
     return HISA_OK;
 }
 

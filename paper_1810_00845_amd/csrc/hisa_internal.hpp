@@ -239,6 +239,42 @@ int moddown_add_fp(hisa_ctx* ctx, const u64* acc, size_t B, int l, const u64* ad
 // exact integer nearest to the double v (ties away from zero), reduced modulo q
 u64 double_to_residue(double v, u64 q);
 
+// ---- tensors (layers.hip), shared with the sequence layers (sequence.hip) ----
+static inline uint32_t t_ci(const hisa_tensor* t) { return t->c_inner ? t->c_inner : 1; }
+static inline size_t t_per(const hisa_tensor* t) { return ((size_t)t->channels + t_ci(t) - 1) / t_ci(t); }
+static inline size_t t_ncts(const hisa_tensor* t) { return (size_t)t->batch * t_per(t); }
+// slot of the last element of a ciphertext
+static inline u64 t_last(const hisa_tensor* t) {
+    return (u64)t->offset + (u64)(t_ci(t) - 1) * t->c_stride + (u64)(t->height - 1) * t->h_stride +
+           (u64)(t->width - 1) * t->w_stride;
+}
+int check_tensor(hisa_ctx* ctx, const hisa_tensor* t);
+void free_handles(hisa_ctx* ctx, std::vector<hisa_ct*>& v);
+int32_t norm_step(const hisa_ctx* ctx, i64 r);      // modulo the slots, from 0
+int write_steps(const std::vector<int32_t>& all, int32_t* steps, size_t cap, size_t* n);
+std::vector<uint32_t> tensor_slots(const hisa_tensor* t);   // of the elements of one ciphertext, channel-major
+int encode_sparse_batch(hisa_ctx* ctx, const std::vector<uint32_t>& slots, const double* values, size_t n_pts, double scale, int limbs,
+                        u64* out);
+int coeffs_to_plain_batch(hisa_ctx* ctx, const int64_t* host, size_t n_pts, int limbs, u64* out, bool ext = false);
+void fill_out_meta(hisa_tensor* out, uint32_t batch, uint32_t channels, uint32_t h, uint32_t w, uint32_t hs, uint32_t ws, uint32_t off,
+                   uint32_t clean, uint32_t c_inner = 1, uint32_t c_stride = 0);
+int mask_run(hisa_ctx* ctx, const hisa_tensor* in, const u64* masks, double mask_scale, std::vector<hisa_ct*>& xs);
+int mask_finish(hisa_ctx* ctx, const hisa_tensor* in, std::vector<hisa_ct*>& xs, hisa_tensor* out);
+
+#define FUSED_PATH "the fused key-switch path (N >= 2^12, every prime below 2^50, dnum <= 8)"
+// Products of rotated ciphertexts before the division by P (hisa_api.hip).  The key from s * sigma_g(s), which
+// hisa_gen_rot_mul_keys makes beside the rotation's own, has this identifier.
+inline u64 product_key_id(u64 galois) { return ((u64)1 << 32) | galois; }
+u64 galois_of(const hisa_ctx* ctx, int32_t steps);   // 0: a multiple of the slots
+// HISA_ERR_NO_KEY unless both keys of the amount are there (a dry run notes the amount instead)
+int product_keys_present(hisa_ctx* ctx, int32_t steps);
+// a sigma(b) from its four products: pairs [n][2][l][N] holds a0 sigma(b1) and a1 sigma(b1), plain [n][2][l][N] a0 sigma(b0) and
+// a1 sigma(b0) with whatever else is to be added; out [n][2][l - 1][N] = (plain + both key switches) / q_{l-1}, one division
+int rotated_products_fp(hisa_ctx* ctx, const u64* pairs, const u64* plain, size_t n, int l, int32_t steps, u64* out);
+// three-polynomial ciphertexts -> two polynomials at the same level: [n][3][l][N] -> out [n][2][l][N]
+int relinearize_fp(hisa_ctx* ctx, const u64* cts3, size_t n, int l, u64* out);
+int rescale_fp(hisa_ctx* ctx, const u64* in, size_t n_polys, int l, u64* out);   // [n_polys][l][N] -> [n_polys][l - 1][N]
+
 // Optional per-kernel timing with HIP events on the launch stream (off by default; the benchmark
 // turns it on for a separate pass).  One scope brackets one kernel launch.
 void prof_begin(const char* kernel, hipStream_t st);
@@ -470,6 +506,12 @@ hipError_t launch_inner_product_sum_fp(const FpPrime* fprimes, const double* ext
                                        u64* acc, u64 acc_bs, u64 n_batch, int shared_input, const u64* c0_src, const u64* plain,
                                        u64 plain_bs, const u64* pmod, int log_n, hipStream_t st);
 
+// acc[b] [2][l + K][N] = the inner products of the two polynomials of pair b, whose extended digits are entries 2 b and 2 b + 1 of ext and
+// whose own digits lie in `pairs` [n][2][l][N], with key and key2, plus P (pmod) times plain [n][2][l][N] on the limbs of q
+hipError_t launch_pair_inner_fp(const FpPrime* fprimes, const double* ext, int digits, int l, int K, int L, int alpha, const u64* key,
+                                const u64* key2, int total, const u64* pairs, const u64* plain, const u64* pmod, u64* acc, u64 n_pairs,
+                                int log_n, hipStream_t st);
+
 // sampling (counter-based generator, both sides of the parity tests implement it)
 hipError_t launch_sample_uniform(const PrimeConst* primes, u64 seed, u64 kind, u64 ctr, const PolyMap& map, int n_polys,
                                  u64 batch_stride, u64 ctr_step, u64* out, int log_n, hipStream_t st);
@@ -501,6 +543,7 @@ hipError_t launch_decrypt(const PrimeConst* primes, const u64* secret, const u64
 hipError_t launch_key_combine(const PrimeConst* primes, const u64* secret, const u64* target, const u64* e,
                               const u64* pmod_all, u64* key_digit, int total, int L, int alpha, int digit, int log_n,
                               hipStream_t st);
+hipError_t launch_pointwise_mul(const PrimeConst* primes, const u64* a, const u64* b, u64* out, int total, int log_n, hipStream_t st);
 hipError_t launch_pointwise_square(const PrimeConst* primes, const u64* s, u64* out, int total, int log_n, hipStream_t st);
 hipError_t launch_automorph_ntt(const u64* in, u64 in_bs, u64* out, u64 out_bs, u64 galois, int n_polys, u64 n_batch,
                                 int log_n, hipStream_t st);

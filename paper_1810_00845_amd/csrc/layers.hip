@@ -1048,15 +1048,6 @@ static hipError_t launch_plain_mac(hisa_ctx* ctx, const PrimeConst* primes, cons
 // helpers
 // ---------------------------------------------------------------------------
 // channels per ciphertext (0 in a zero-initialised struct means HW-tiling), ciphertexts per image, ciphertexts in all
-static inline uint32_t t_ci(const hisa_tensor* t) { return t->c_inner ? t->c_inner : 1; }
-static inline size_t t_per(const hisa_tensor* t) { return ((size_t)t->channels + t_ci(t) - 1) / t_ci(t); }
-static inline size_t t_ncts(const hisa_tensor* t) { return (size_t)t->batch * t_per(t); }
-// slot of the last element of a ciphertext
-static inline u64 t_last(const hisa_tensor* t) {
-    return (u64)t->offset + (u64)(t_ci(t) - 1) * t->c_stride + (u64)(t->height - 1) * t->h_stride +
-           (u64)(t->width - 1) * t->w_stride;
-}
-
 static int check_layout(hisa_ctx* ctx, const hisa_tensor* t) {
     if (!t || !t->cts || t->batch == 0 || t->channels == 0 || t->height == 0 || t->width == 0)
         return fail(ctx, HISA_ERR_ARG, "empty tensor");
@@ -1065,7 +1056,7 @@ static int check_layout(hisa_ctx* ctx, const hisa_tensor* t) {
     return HISA_OK;
 }
 
-static int check_tensor(hisa_ctx* ctx, const hisa_tensor* t) {
+int check_tensor(hisa_ctx* ctx, const hisa_tensor* t) {
     if (!ctx) return HISA_ERR_ARG;
     TRY(check_layout(ctx, t));
     return check_batch_shape(ctx, (const hisa_ct* const*)t->cts, t_ncts(t), 2);
@@ -1077,12 +1068,12 @@ static int require_hw_tiling(hisa_ctx* ctx, const hisa_tensor* t, const char* wh
     return HISA_OK;
 }
 
-static void free_handles(hisa_ctx* ctx, std::vector<hisa_ct*>& v) {
+void free_handles(hisa_ctx* ctx, std::vector<hisa_ct*>& v) {
     for (hisa_ct* c : v) hisa_free(ctx, c);
     v.clear();
 }
 
-static int32_t norm_step(const hisa_ctx* ctx, i64 r) {
+int32_t norm_step(const hisa_ctx* ctx, i64 r) {
     const i64 slots = ctx->N / 2;
     r %= slots;
     if (r < 0) r += slots;
@@ -1154,7 +1145,7 @@ static i64 conv_wrap_amount(const hisa_ctx* ctx, const hisa_tensor* in) {
     return 2 * span <= slots ? (i64)span : -1;
 }
 
-static int write_steps(const std::vector<int32_t>& all, int32_t* steps, size_t cap, size_t* n) {
+int write_steps(const std::vector<int32_t>& all, int32_t* steps, size_t cap, size_t* n) {
     std::set<int32_t> uniq;
     for (int32_t s : all)
         if (s != 0) uniq.insert(s);
@@ -1260,7 +1251,7 @@ static std::vector<uint32_t> plane_slots(uint32_t h, uint32_t w, uint32_t hs, ui
 }
 
 // slots of the elements of one ciphertext, channel-major
-static std::vector<uint32_t> tensor_slots(const hisa_tensor* t) {
+std::vector<uint32_t> tensor_slots(const hisa_tensor* t) {
     std::vector<uint32_t> s;
     for (uint32_t c = 0; c < t_ci(t); c++)
         for (uint32_t v : plane_slots(t->height, t->width, t->h_stride, t->w_stride, t->offset + c * t->c_stride)) s.push_back(v);
@@ -1270,8 +1261,8 @@ static std::vector<uint32_t> tensor_slots(const hisa_tensor* t) {
 // Encodes n_pts slot vectors that are non-zero only on `slots` (values[n_pts][slots.size()], host) into
 // NTT-form plaintexts out[n_pts][limbs][N] (device).  Here and in encode_piecewise_batch coefficient N - k is minus
 // coefficient k, as for any real vector, exactly: only half of them are computed.
-static int encode_sparse_batch(hisa_ctx* ctx, const std::vector<uint32_t>& slots, const double* values, size_t n_pts,
-                               double scale, int limbs, u64* out) {
+int encode_sparse_batch(hisa_ctx* ctx, const std::vector<uint32_t>& slots, const double* values, size_t n_pts,
+                        double scale, int limbs, u64* out) {
     const size_t nnz = slots.size(), n = ctx->N;
     std::vector<uint32_t> g(nnz);
     const uint32_t mask = 2 * ctx->N - 1;
@@ -1376,7 +1367,7 @@ static int encode_piecewise_batch(hisa_ctx* ctx, const std::vector<std::vector<u
 }
 
 // host signed coefficients [n_pts][N] -> NTT-form plaintexts out[n_pts][limbs][N]
-static int coeffs_to_plain_batch(hisa_ctx* ctx, const int64_t* host, size_t n_pts, int limbs, u64* out, bool ext = false) {
+int coeffs_to_plain_batch(hisa_ctx* ctx, const int64_t* host, size_t n_pts, int limbs, u64* out, bool ext) {
     const size_t n = ctx->N, tot = limbs + (ext ? ctx->K : 0);
     for (size_t p0 = 0; p0 < n_pts; p0 += 4096) {
         const size_t cnt = std::min<size_t>(4096, n_pts - p0);
@@ -1395,8 +1386,8 @@ static u64 mod_i64(i64 v, u64 q) {
     return m ? q - m : 0;
 }
 
-static void fill_out_meta(hisa_tensor* out, uint32_t batch, uint32_t channels, uint32_t h, uint32_t w, uint32_t hs,
-                          uint32_t ws, uint32_t off, uint32_t clean, uint32_t c_inner = 1, uint32_t c_stride = 0) {
+void fill_out_meta(hisa_tensor* out, uint32_t batch, uint32_t channels, uint32_t h, uint32_t w, uint32_t hs,
+                   uint32_t ws, uint32_t off, uint32_t clean, uint32_t c_inner, uint32_t c_stride) {
     out->batch = batch; out->channels = channels; out->height = h; out->width = w;
     out->h_stride = hs; out->w_stride = ws; out->offset = off; out->clean = clean;
     out->c_inner = c_inner; out->c_stride = c_stride;
@@ -2683,7 +2674,7 @@ static int rotate_add_chain(hisa_ctx* ctx, std::vector<hisa_ct*>& xs, const std:
 // The masking multiply (Sec. "Homomorphic Tensor Operations", SAME-padding paragraph): xs = rescale(in * mask), the
 // mask being 0/1 on the element slots at the scale of the last modulus.  masks: NTT-form plaintexts [per][l][N];
 // ciphertext j of every image takes mask j (they differ only where a last ciphertext holds fewer channels).
-static int mask_run(hisa_ctx* ctx, const hisa_tensor* in, const u64* masks, double mask_scale, std::vector<hisa_ct*>& xs) {
+int mask_run(hisa_ctx* ctx, const hisa_tensor* in, const u64* masks, double mask_scale, std::vector<hisa_ct*>& xs) {
     const uint32_t B = in->batch, per = (uint32_t)t_per(in), l = in->cts[0]->limbs;
     const size_t n_in = (size_t)B * per, n = ctx->N;
     if (l < 2) return fail(ctx, HISA_ERR_DEPTH_EXHAUSTED, "the masking multiply needs a level to rescale into");
@@ -2715,7 +2706,7 @@ static int encode_masks(hisa_ctx* ctx, const hisa_tensor* t, double scale, uint3
     return encode_sparse_batch(ctx, tensor_slots(t), ones.data(), per, scale, (int)l, out);
 }
 
-static int mask_finish(hisa_ctx* ctx, const hisa_tensor* in, std::vector<hisa_ct*>& xs, hisa_tensor* out) {
+int mask_finish(hisa_ctx* ctx, const hisa_tensor* in, std::vector<hisa_ct*>& xs, hisa_tensor* out) {
     for (size_t i = 0; i < xs.size(); i++) out->cts[i] = xs[i];
     fill_out_meta(out, in->batch, in->channels, in->height, in->width, in->h_stride, in->w_stride, in->offset, 1, t_ci(in),
                   in->c_stride);

@@ -78,6 +78,11 @@ class ConvGeom(C.Structure):
                 ("mode", C.c_uint32), ("shared_moddown", C.c_uint32), ("chw_schedule", C.c_uint32)]
 
 
+class NormGeom(C.Structure):
+    _fields_ = [("groups", C.c_uint32), ("iterations", C.c_uint32), ("eps", C.c_double), ("var_lo", C.c_double), ("var_hi", C.c_double),
+                ("act_ratio", C.c_double), ("act", C.c_uint32), ("reserved", C.c_uint32)]
+
+
 _lib = None
 
 
@@ -219,6 +224,10 @@ class Context:
     def gen_rot_keys(self, left_steps):
         arr = (C.c_int32 * len(left_steps))(*[int(s) for s in left_steps])
         self._ck(load().hisa_gen_rot_keys(self._vp, arr, C.c_size_t(len(left_steps))))
+
+    def gen_rot_mul_keys(self, left_steps):
+        arr = (C.c_int32 * max(1, len(left_steps)))(*[int(s) for s in left_steps])
+        self._ck(load().hisa_gen_rot_mul_keys(self._vp, arr, C.c_size_t(len(left_steps))))
 
     def galois_elt(self, steps):
         g = C.c_uint64()
@@ -630,6 +639,74 @@ class Context:
     def poly2_act(self, t, a, b):
         return self._layer("hisa_poly2_act", t, len(t.cts), C.c_double(a), C.c_double(b))
 
+    # ---- layers of sequence models ----
+    def recurrence(self, gates, x, reverse=False):
+        """h[t] = x[t] + gates[t] h[t - 1] along the width (reverse: h[t + 1]); gates zero at the first token (recurrence_gates)."""
+        xs, _arr = x._struct()
+        return self._layer("hisa_recurrence", gates, len(x.cts), C.byref(xs), C.c_uint32(int(reverse)))
+
+    def recurrence_step(self, gates, state, x):
+        """One token: x + gates * state."""
+        (ss, _a), (xs, _b) = state._struct(), x._struct()
+        return self._layer("hisa_recurrence_step", gates, len(x.cts), C.byref(ss), C.byref(xs))
+
+    def recurrence_grad(self, gates, h, grad, reverse=False):
+        """(gradient of x, gradient of the gates) from the states h of recurrence(gates, x) and their gradient."""
+        structs = [t._struct() for t in (gates, h, grad)]
+        outs = [CipherTensor(self, [None] * len(t.cts), 0, 0, 0, 0, 0, 0, 0, 0, 1, 0) for t in (grad, gates)]
+        out_structs = [o._struct() for o in outs]
+        self._ck(load().hisa_recurrence_grad(self._vp, *[C.byref(st) for st, _ in structs], C.c_uint32(int(reverse)),
+                                             *[C.byref(st) for st, _ in out_structs]))
+        for o, (st, arr) in zip(outs, out_structs):
+            o._adopt(st, arr)
+        return tuple(outs)
+
+    def recurrence_gates(self, gates, reverse=False):
+        """Gates with zero at the token that has no predecessor (and beside the elements), one level lower."""
+        return self._layer("hisa_recurrence_gates", gates, len(gates.cts), C.c_uint32(int(reverse)))
+
+    def recurrence_gates_fixed(self, gates, mask_coeffs, mask_scale):
+        mc = np.ascontiguousarray(mask_coeffs, dtype=np.int64)
+        assert mc.shape == (-(-gates.channels // gates.c_inner), self.N)
+        return self._layer("hisa_recurrence_gates_fixed", gates, len(gates.cts), mc.ctypes.data_as(C.POINTER(C.c_int64)), C.c_double(mask_scale))
+
+    def recurrence_rot_steps(self, like, reverse=False, backward=False):
+        return self._steps("hisa_recurrence_rot_steps", like, C.c_uint32(int(reverse)), C.c_uint32(int(backward)))
+
+    @staticmethod
+    def _norm_geom(groups, eps, var_lo, var_hi, iterations, act_ratio):
+        return NormGeom(groups, iterations, eps, var_lo, var_hi, 0.0 if act_ratio is None else act_ratio, 0 if act_ratio is None else 1, 0)
+
+    def group_norm_prepare(self, like, gamma, beta, groups, eps, var_lo, var_hi, iterations, act_ratio=None):
+        """Encodes gamma and beta (per channel, or None) for tensors laid out like `like`; act_ratio: y^2 + act_ratio y behind the
+        normalisation.  Returns a plan for group_norm_apply (free with group_norm_plan_free)."""
+        g, b = (None if v is None else np.ascontiguousarray(v, dtype=np.float64) for v in (gamma, beta))
+        assert all(v is None or v.shape == (like.channels,) for v in (g, b))
+        st, _arr = like._struct()
+        plan = C.c_void_p()
+        self._ck(load().hisa_group_norm_prepare(self._vp, C.byref(st), _dp(g), _dp(b),
+                                                C.byref(self._norm_geom(groups, eps, var_lo, var_hi, iterations, act_ratio)), C.byref(plan)))
+        return plan
+
+    def group_norm_prepare_fixed(self, like, gamma_coeffs, gamma_scale, beta_coeffs, groups, eps, var_lo, var_hi, iterations, act_ratio=None):
+        g, b = (np.ascontiguousarray(v, dtype=np.int64) for v in (gamma_coeffs, beta_coeffs))
+        assert g.shape == b.shape == (-(-like.channels // like.c_inner), self.N)
+        st, _arr = like._struct()
+        plan, i64p = C.c_void_p(), C.POINTER(C.c_int64)
+        self._ck(load().hisa_group_norm_prepare_fixed(self._vp, C.byref(st), g.ctypes.data_as(i64p), C.c_double(gamma_scale), b.ctypes.data_as(i64p),
+                                                      C.byref(self._norm_geom(groups, eps, var_lo, var_hi, iterations, act_ratio)),
+                                                      C.byref(plan)))
+        return plan
+
+    def group_norm_apply(self, t, plan):
+        return self._layer("hisa_group_norm_apply", t, len(t.cts), plan)
+
+    def group_norm_plan_free(self, plan):
+        self._ck(load().hisa_group_norm_plan_free(self._vp, plan))
+
+    def group_norm_rot_steps(self, t):
+        return self._steps("hisa_group_norm_rot_steps", t)
+
     def _steps(self, fn, t, *args):
         st, _arr = t._struct()
         buf = (C.c_int32 * 1024)()      # a CHW-tiled convolution alone can ask for 257 amounts
@@ -688,6 +765,11 @@ class Context:
         out = np.zeros((self.dnum, 2, self.L + self.K, self.N), dtype=np.uint64)
         self._ck(load().hisa_key_export(self._vp, C.c_uint64(key_id), out.ctypes.data_as(C.POINTER(C.c_uint64))))
         return out
+
+    def key_import(self, key_id, key):
+        k = np.ascontiguousarray(key, dtype=np.uint64)
+        assert k.shape == (self.dnum, 2, self.L + self.K, self.N)
+        self._ck(load().hisa_key_import(self._vp, C.c_uint64(key_id), k.ctypes.data_as(C.POINTER(C.c_uint64))))
 
     def secret_export(self):
         out = np.zeros(self.N, dtype=np.int64)
