@@ -648,7 +648,7 @@ __device__ __forceinline__ void rows_forward(const ConvertArgs& a, int n_tasks, 
 struct OneStep {};
 template <int K3, int MODE, bool ONCE, class S>
 __device__ __forceinline__ void rows_inner(const ConvertArgs& a, const InnerArgs& g, const S& s, int n_tasks, double* lds_all) {
-    constexpr bool STEPS = !std::is_same<S, OneStep>::value;
+    constexpr bool STEPS = std::is_same<S, StepArgs>::value, PAIR = std::is_same<S, PairArgs>::value;
     const int per = (n_tasks + 7) >> 3;
     const int task = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
     if (task >= n_tasks) return;
@@ -679,7 +679,9 @@ __device__ __forceinline__ void rows_inner(const ConvertArgs& a, const InnerArgs
         if (d < a.n_digits) {
             double v[16];
             if (x >= a.dg[d].own_lo && x < a.dg[d].own_lo + a.dg[d].own_n) {
-                load_row_through<K3>(v, g.own + ct * g.own_bs + (u64)x * n, galois, row, lane);
+                const u64* own = g.own + ct * g.own_bs + (u64)x * n;
+                if constexpr (PAIR) own += d < s.half ? 0 : s.own2;
+                load_row_through<K3>(v, own, galois, row, lane);
                 from_residues(v);
 #pragma unroll
                 for (int r = 0; r < 16; r++) lds[at + ROW_REG(r)] = v[r];
@@ -702,9 +704,18 @@ __device__ __forceinline__ void rows_inner(const ConvertArgs& a, const InnerArgs
             }
         }
         SCHED_FENCE();
-        const double* key_p = (const double*)key + (((u64)d0 * 2 + poly) * a.total + prime) * n + row * 1024u;
         const bool two = d0 + 1 < a.n_digits;
-        const rsrc_t k0r = make_rsrc(key_p, 8192u), k1r = make_rsrc(two ? key_p + (u64)2 * a.total * n : key_p, 8192u);
+        const double *key_p, *key_q;
+        if constexpr (PAIR) {
+            auto key_of = [&](int d) {
+                return (const double*)(d < s.half ? key : s.key2) + (((u64)(d < s.half ? d : d - s.half) * 2 + poly) * a.total + prime) * n + row * 1024u;
+            };
+            key_p = key_of(d0); key_q = key_of(d0 + 1);
+        } else {
+            key_p = (const double*)key + (((u64)d0 * 2 + poly) * a.total + prime) * n + row * 1024u;
+            key_q = two ? key_p + (u64)2 * a.total * n : key_p;
+        }
+        const rsrc_t k0r = make_rsrc(key_p, 8192u), k1r = make_rsrc(key_q, 8192u);
         double k0[16], k1[16];
         load_key_row<ONCE>(k0, k0r, lane);
         // (also without a second digit, then of the first: words left undefined would stay live through the loop)
@@ -897,8 +908,9 @@ __device__ __forceinline__ void wide_rows_forward(const ConvertArgs& a, int task
 // per polynomial too, for launches that leave compute units idle (the rule stands at the launch): the digits' rows are transformed for
 // either, and what follows them is left to four waves that have waited with keys and twiddles in registers (with four digits, to those of
 // the first).
-template <int K3, int MODE>
-__device__ __forceinline__ void wide_rows_inner(const ConvertArgs& a, const InnerArgs& g, int task, double* lds) {
+template <int K3, int MODE, class S>
+__device__ __forceinline__ void wide_rows_inner(const ConvertArgs& a, const InnerArgs& g, const S& s, int task, double* lds) {
+    constexpr bool PAIR = std::is_same<S, PairArgs>::value;
     const uint32_t t = threadIdx.x & (WIDE_NT - 1);
     const int part = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / WIDE_NT));
     const uint32_t entry = (uint32_t)task >> g.split, unit = entry / a.n_entries;
@@ -919,7 +931,9 @@ __device__ __forceinline__ void wide_rows_inner(const ConvertArgs& a, const Inne
     WideTwiddles w;
     double* slot = lds + part * WIDE_LDS;
     if (own) {
-        wide_load<K3>(v, g.own + b * g.own_bs + (u64)x * n, g.galois, row, t);
+        const u64* from = g.own + b * g.own_bs + (u64)x * n;
+        if constexpr (PAIR) from += part < s.half ? 0 : s.own2;
+        wide_load<K3>(v, from, g.galois, row, t);
     } else if (mine) {
         const rsrc_t src = make_rsrc((const double*)a.out + b * a.out_bs + (u64)(a.dg[part].out_pos0 + x) * n + row * 1024u, 8192u);
 #pragma unroll
@@ -930,8 +944,13 @@ __device__ __forceinline__ void wide_rows_inner(const ConvertArgs& a, const Inne
     else if (!own || MODE == FP_FWD_CONV_SUB) wide_twiddles(w, a.sfwd, a.table_stride, prime, row, t, q);
     if (sums) {
 #pragma unroll
-        for (int d = 0; d < WIDE_DIGITS; d++)
-            if (d < a.n_digits) wide_load<K3>(k[d], g.key + (((u64)d * 2 + poly) * a.total + prime) * n, 0, row, t);
+        for (int d = 0; d < WIDE_DIGITS; d++) {
+            if (d >= a.n_digits) break;
+            const u64* key = g.key + (((u64)d * 2 + poly) * a.total + prime) * n;
+            if constexpr (PAIR)
+                if (d >= s.half) key = s.key2 + (((u64)(d - s.half) * 2 + poly) * a.total + prime) * n;
+            wide_load<K3>(k[d], key, 0, row, t);
+        }
         if (with_add) wide_load<K3>(add, g.add + b * g.add_bs + (u64)poly * g.add_ps + (u64)x * n, g.galois, row, t);
         if (MODE == FP_FWD_CONV_SUB) {
 #pragma unroll
@@ -1297,7 +1316,7 @@ __global__ __launch_bounds__(fp_inner(MODE) ? WIDE_DIGITS * WIDE_NT : WIDE_NT, 4
     const int task = wide_task(n_tasks);
     if (task < 0) return;
     if constexpr (MODE == FP_INV_TO_Y) wide_rows_inverse<K3>(a, task, wide_lds);
-    else if constexpr (fp_inner(MODE)) wide_rows_inner<K3, MODE>(a, g, task, wide_lds);
+    else if constexpr (fp_inner(MODE)) wide_rows_inner<K3, MODE>(a, g, OneStep{}, task, wide_lds);
     else wide_rows_forward<K3, MODE>(a, task, wide_lds);
 }
 
@@ -1638,4 +1657,61 @@ static hipError_t launch_step_rows_once(int mode, dim3 grid, const ConvertArgs& 
     ONCE_CASE(2, FP_FWD_CONV_SUB) ONCE_CASE(3, FP_FWD_CONV_SUB) ONCE_CASE(4, FP_FWD_CONV_SUB) ONCE_CASE(5, FP_FWD_CONV_SUB)
 #undef ONCE_CASE
     return hipErrorInvalidValue;
+}
+
+// ---- pairs: two polynomials with a key each, one accumulator, one division (products of rotated ciphertexts) ----
+// The digits of the second polynomial stand behind those of the first (a.n_digits counts both, at most FP_MAX_DIGITS); the same rows as
+// above otherwise.  Two waves a task have both something to transform in every round where one polynomial of three digits leaves
+// one of them idle in the second.
+template <int K3, int MODE>
+__global__ __launch_bounds__(128, 4) void inner_product_pair_rows_kernel(ConvertArgs a, InnerArgs g, PairArgs s, int n_tasks) {
+    __shared__ double lds[2 * ROW_LDS];
+    rows_inner<K3, MODE, false>(a, g, s, n_tasks, lds);
+}
+template <int K3, int MODE>
+__global__ __launch_bounds__(WIDE_DIGITS * WIDE_NT, 4) void inner_product_pair_wide_kernel(ConvertArgs a, InnerArgs g, PairArgs s, int n_tasks) {
+    extern __shared__ double wide_lds[];
+    const int task = wide_task(n_tasks);
+    if (task >= 0) wide_rows_inner<K3, MODE>(a, g, s, task, wide_lds);
+}
+
+template <int K3, int MODE>
+static hipError_t launch_pair_k3(const ConvertArgs& a, const InnerArgs& g_in, const PairArgs& s, u64 tasks, hipStream_t st) {
+    if (tasks <= wide_inner_tasks(a.n_digits)) {
+        InnerArgs g = g_in;
+        g.split = 2 * tasks <= WIDE_SPLIT;
+        const unsigned rows = g.split ? std::min((unsigned)a.n_digits + 1, (unsigned)WIDE_DIGITS) : (unsigned)a.n_digits;
+        tasks <<= g.split;
+        ProfScope prof__("inner_product_pair_wide_kernel", st);
+        hipLaunchKernelGGL((inner_product_pair_wide_kernel<K3, MODE>), dim3((unsigned)((tasks + 7) / 8 * 8)), dim3(rows * WIDE_NT),
+                           rows * WIDE_LDS * 8, st, a, g, s, (int)tasks);
+    } else {
+        ProfScope prof__("inner_product_pair_rows_kernel", st);
+        hipLaunchKernelGGL((inner_product_pair_rows_kernel<K3, MODE>), dim3((unsigned)((tasks + 7) / 8 * 8)), dim3(128), 0, st, a, g_in, s, (int)tasks);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_inner_pair_rows_fp(int mode, const ConvertArgs& a, const InnerArgs& g, const PairArgs& s, hipStream_t st) {
+    DRY_RUN_RETURN();
+    u64 targets = 0;
+    const u64 n = (u64)1 << a.log_n;
+    if (a.n_entries == 0 || !convert_args_ok(a, &targets) || s.half < 1 || a.n_digits != 2 * s.half) return hipErrorInvalidValue;
+    if (!g.key || !s.key2 || !g.own || !g.c1 || g.galois || g.n_acc < 1 || g.n_acc >= a.ext_limbs || g.n_acc > a.l) return hipErrorInvalidValue;
+    if (g.x_begin < 0 || g.x_begin >= g.x_end || g.x_end > a.ext_limbs || g.own_bs < s.own2 + (u64)a.l * n || s.own2 < (u64)a.l * n)
+        return hipErrorInvalidValue;
+    if (g.add_polys != 2 || !g.add || g.add_bs < 2 * (u64)a.l * n || g.add_ps < (u64)a.l * n || a.out_bs < (u64)a.n_digits * a.ext_limbs * n)
+        return hipErrorInvalidValue;
+    const u64 tasks = ((u64)(g.x_end - g.x_begin) * a.n_entries) << (a.log_n - 10);
+    if (tasks > 0x7fffff00u) return hipErrorInvalidValue;
+    if (mode == FP_INV_D_TO_Y ? (g.x_begin < g.n_acc && !g.acc) || (g.x_end > g.n_acc && !g.down) : mode != FP_FWD_CONV_SUB || g.x_end > g.n_acc || !g.out)
+        return hipErrorInvalidValue;
+#define PAIR_CASE(K3)                                                                                      \
+    case 10 + K3:                                                                                          \
+        return mode == FP_INV_D_TO_Y ? launch_pair_k3<K3, FP_INV_D_TO_Y>(a, g, s, tasks, st) : launch_pair_k3<K3, FP_FWD_CONV_SUB>(a, g, s, tasks, st);
+    switch (a.log_n) {
+        PAIR_CASE(2) PAIR_CASE(3) PAIR_CASE(4) PAIR_CASE(5)
+        default: return hipErrorInvalidValue;
+    }
+#undef PAIR_CASE
 }

@@ -1772,14 +1772,17 @@ extern "C" int hisa_rot_left_sum_batch(hisa_ctx* ctx, const hisa_ct* const* in, 
 // C, D and E: the inner products of `entries` key switches on the digits that c names, and the division by P.
 // g.acc != null ([entries][2][l][N] doubles): the limbs of q are summed in launch C too and E only subtracts -- the shorter
 // chain of launches where they do not fill the chip.
-static int key_switch_divide_fp(hisa_ctx* ctx, ConvertArgs& c, InnerArgs& g, const Division& by, const StepArgs* steps, int l, size_t entries,
-                                u64* out) {
+static int key_switch_divide_fp(hisa_ctx* ctx, ConvertArgs& c, InnerArgs& g, const Division& by, const StepArgs* steps, const PairArgs* pair, int l,
+                                size_t entries, u64* out) {
     const size_t n = ctx->N;
     const int ext_limbs = l + (int)ctx->K, left = by.n_acc, sources = ext_limbs - left;
     g.n_acc = left; g.c1 = by.c1; g.c2 = by.c2;
     g.x_begin = g.acc ? 0 : left; g.x_end = ext_limbs;
     c.n_entries = (unsigned)entries;
-    HIP_TRY(ctx, launch_inner_rows_fp(FP_INV_D_TO_Y, c, g, steps, ctx->stream));
+    auto inner = [&](int mode) {
+        return pair ? launch_inner_pair_rows_fp(mode, c, g, *pair, ctx->stream) : launch_inner_rows_fp(mode, c, g, steps, ctx->stream);
+    };
+    HIP_TRY(ctx, inner(FP_INV_D_TO_Y));
     ConvertArgs m = convert_base(ctx, l, entries * 2);      // entries are (ciphertext, b|a) pairs
     m.src_pos0 = left; m.n_src = sources; m.mid = g.down;
     m.n_digits = 1; m.dg[0] = {by.hat, 0, sources, 0, 0, 0}; m.ext_limbs = left; m.out = out; m.out_bs = (u64)left * n;
@@ -1789,7 +1792,7 @@ static int key_switch_divide_fp(hisa_ctx* ctx, ConvertArgs& c, InnerArgs& g, con
         HIP_TRY(ctx, launch_forward_rows_fp(FP_FWD_SUB, m, ctx->stream));
     } else {
         g.out = out; g.x_begin = 0; g.x_end = left;
-        HIP_TRY(ctx, launch_inner_rows_fp(FP_FWD_CONV_SUB, c, g, steps, ctx->stream));
+        HIP_TRY(ctx, inner(FP_FWD_CONV_SUB));
     }
     return HISA_OK;
 }
@@ -1811,7 +1814,7 @@ static int key_switch_fused_fp(hisa_ctx* ctx, const u64* d, u64 d_bs, u64 galois
     g.key = key.data; g.own = d; g.own_bs = d_bs; g.galois = galois;
     g.add = add; g.add_bs = add_bs; g.add_ps = (u64)l * n; g.add_polys = add ? add_polys : 0;
     g.acc = acc; g.down = down;
-    return key_switch_divide_fp(ctx, c, g, by, nullptr, l, B, out);
+    return key_switch_divide_fp(ctx, c, g, by, nullptr, nullptr, l, B, out);
 }
 
 // Keeping the accumulators in registers until the division's transform is there saves a quarter of the memory traffic, but makes
@@ -1846,7 +1849,7 @@ static int key_switch_finish_steps_fp(hisa_ctx* ctx, const FpExt& x, const u64* 
     StepArgs st = {};
     st.step_B = (unsigned)B;
     for (int s = 0; s < n_steps; s++) { st.steps.key[s] = keys[s]->data; st.steps.galois[s] = (uint32_t)galois[s]; }
-    return key_switch_divide_fp(ctx, c, g, by, &st, l, E, out);
+    return key_switch_divide_fp(ctx, c, g, by, &st, nullptr, l, E, out);
 }
 
 static int key_switch_core_fp(hisa_ctx* ctx, const u64* d, u64 d_bs, u64 galois, size_t B, int l, const SwitchKey& key,
@@ -1924,8 +1927,35 @@ int rotated_products_fp(hisa_ctx* ctx, const u64* pairs, const u64* plain, size_
     const size_t n = ctx->N;
     const int K = (int)ctx->K, ext_limbs = l + K;
     FpExt x(ctx, 2 * n_pairs, l, K, (int)ctx->alpha);
+    if (!x.ok()) return HISA_ERR_OOM;
+    if (2 * x.digits <= FP_MAX_DIGITS) {      // five launches, as key_switch_fused_fp's
+        Division by;
+        TRY(division_by_p_and_last(ctx, l, &by));
+        const bool stored = store_accumulators(ctx, n_pairs, ext_limbs);
+        const size_t poly = n_pairs * 2 * n * sizeof(double);
+        Temp acc(ctx, poly * (size_t)by.n_acc, stored), down(ctx, poly * (size_t)(ext_limbs - by.n_acc));
+        if ((stored && !acc.ok()) || !down.ok()) return HISA_ERR_OOM;
+        double *post_q, *post_p;
+        TRY(fp_post_tables(ctx, l, &post_q, &post_p, false));
+        ConvertArgs c = convert_base(ctx, l, 2 * n_pairs);
+        TRY(modup_digits(ctx, c, x, false));
+        c.in = pairs; c.in_bs = (u64)l * n; c.post = post_q;
+        HIP_TRY(ctx, launch_inverse_rows_fp(c, ctx->stream));
+        HIP_TRY(ctx, launch_columns_fp(FP_FWD_CONV, c, ctx->stream));
+        c.n_entries = (unsigned)n_pairs; c.n_digits = 2 * x.digits; c.out_bs = 2 * x.ext_bs;
+        for (int d = 0; d < x.digits; d++) {
+            c.dg[x.digits + d] = c.dg[d];
+            c.dg[x.digits + d].out_pos0 += x.digits * ext_limbs;
+        }
+        InnerArgs g = {};
+        g.key = key.data; g.own = pairs; g.own_bs = (u64)2 * l * n;
+        g.add = plain; g.add_bs = (u64)2 * l * n; g.add_ps = (u64)l * n; g.add_polys = 2;
+        g.acc = stored ? acc.as<double>() : nullptr; g.down = down.as<double>();
+        const PairArgs second = {key2.data, (u64)l * n, x.digits};
+        return key_switch_divide_fp(ctx, c, g, by, nullptr, &second, l, n_pairs, out);
+    }
     Temp acc(ctx, n_pairs * 2 * (size_t)ext_limbs * n * sizeof(u64));
-    if (!x.ok() || !acc.ok()) return HISA_ERR_OOM;
+    if (!acc.ok()) return HISA_ERR_OOM;
     TRY(key_switch_modup_fp(ctx, pairs, (u64)l * n, 2 * n_pairs, x));
     HIP_TRY(ctx, launch_pair_inner_fp(ctx->tabs.fprimes, x.extp, x.digits, l, K, (int)ctx->L, (int)ctx->alpha, key.data, key2.data,
                                       (int)ctx->total, pairs, plain, ctx->d_pmod, acc.u(), n_pairs, (int)ctx->log_n, ctx->stream));

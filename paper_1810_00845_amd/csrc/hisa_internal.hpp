@@ -434,6 +434,14 @@ struct StepArgs {
     unsigned step_B;
     IpSteps steps;
 };
+// The same for pairs of polynomials with a key each and one accumulator: a.n_digits = 2 half, the digits of the second behind those of the
+// first in an entry of a.out, its own digits own2 words behind the first's, its key key2.
+struct PairArgs {
+    const u64* key2;
+    u64 own2;
+    int half;
+};
+hipError_t launch_inner_pair_rows_fp(int mode, const ConvertArgs& a, const InnerArgs& g, const PairArgs& s, hipStream_t st);
 hipError_t launch_inner_rows_fp(int mode, const ConvertArgs& a, const InnerArgs& g, const StepArgs* steps, hipStream_t st);
 
 // ---- the same division of work in 64-bit integers (convert_int.hip): any ring degree, primes up to 60 bits, any number of
