@@ -1715,3 +1715,145 @@ hipError_t launch_inner_pair_rows_fp(int mode, const ConvertArgs& a, const Inner
     }
 #undef PAIR_CASE
 }
+
+// ---- products of ciphertexts with the inverse rows of what their key switch decomposes ----
+// A workgroup per (limb, row, entry), four waves per polynomial: with b rotated, waves of polynomial u form a_u sigma(b0) + f c_u, which
+// needs no key, and a_u sigma(b1), whose inverse rows they go on with; else the first four form the two polynomials of the result and
+// the others a1 b1 and its inverse rows.
+// Bound by memory (4.4 TB/s of what it cannot do without at 38 products, N = 2^15, 16 limbs), by its chain of loads, products and ten
+// levels where it is small.  As two launches / here: those 38 products 299 / 295 us, one at N = 2^13, 8 limbs 8.0 / 6.5, two rotated at
+// N = 2^15, 21 limbs 20.1 / 16.
+// Ranges: factors canonical, products within 0.875 p, at most four more on a normalised value.
+#define PRODUCT_NT (2 * WIDE_NT)
+template <int K3, bool ROTATED>
+__global__ __launch_bounds__(PRODUCT_NT, 4) void product_rows_kernel(ProductArgs g, int n_tasks) {
+    __shared__ double lds_all[2 * WIDE_LDS];
+    const int task = wide_task(n_tasks);
+    if (task < 0) return;
+    constexpr u64 n = (u64)1 << (10 + K3);
+    const uint32_t t = threadIdx.x & (WIDE_NT - 1), unit = (uint32_t)task / (uint32_t)g.n_entries, entry = (uint32_t)task - unit * (uint32_t)g.n_entries;
+    const int u = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / WIDE_NT));
+    const uint32_t row = unit & ((1u << K3) - 1);
+    const int limb = (int)(unit >> K3);
+    const bool second = entry >= g.n_first;
+    const ProductSide& s = g.s[second ? 1 : 0];
+    const uint32_t e = second ? entry - g.n_first : entry, terms = second ? 1 : g.terms;
+    const Modulus q = modulus(g.fprimes, limb);
+    const u64 lw = (u64)g.limbs * n, limb_at = (u64)limb * n;
+    const bool transforms = ROTATED || u;
+    double x[4] = {}, y[4] = {}, c[4], d[4];
+    WideTwiddles w;
+    if (s.add && (ROTATED || !u)) {
+        const u64* add = s.add + (u64)e * s.add_bs + limb_at;
+        wide_load<K3>(c, add + (ROTATED ? u : 0) * s.add_ps, 0, row, t);
+        if (!ROTATED) wide_load<K3>(d, add + s.add_ps, 0, row, t);
+    }
+    for (uint32_t k = 0; k < terms; k++) {
+        const u64 *a = s.a + (u64)(terms > 1 ? e * terms + k : e / s.a_div) * s.a_bs + limb_at, *b = s.b + (u64)(e * terms + k) * s.b_bs + limb_at;
+        if (ROTATED) {
+            double a_u[4], b0[4], b1[4];
+            wide_load<K3>(a_u, a + u * s.a_ps, 0, row, t);
+            wide_load<K3>(b0, b, g.galois, row, t);
+            wide_load<K3>(b1, b + s.b_ps, g.galois, row, t);
+            if (k == 0) wide_twiddles(w, g.sinv, g.table_stride, limb, row, t, q);
+            wide_from_residues(a_u); wide_from_residues(b0); wide_from_residues(b1);
+#pragma unroll
+            for (int r = 0; r < 4; r++) {
+                x[r] += fp_mulmod(a_u[r], b0[r], q.p, q.pinv);
+                y[r] += fp_mulmod(a_u[r], b1[r], q.p, q.pinv);
+            }
+        } else if (u) {
+            double a1[4], b1[4];
+            wide_load<K3>(a1, a + s.a_ps, 0, row, t);
+            wide_load<K3>(b1, b + s.b_ps, 0, row, t);
+            if (k == 0) wide_twiddles(w, g.sinv, g.table_stride, limb, row, t, q);
+            wide_from_residues(a1); wide_from_residues(b1);
+#pragma unroll
+            for (int r = 0; r < 4; r++) y[r] += fp_mulmod(a1[r], b1[r], q.p, q.pinv);
+        } else {
+            double a0[4], a1[4], b0[4], b1[4];
+            wide_load<K3>(a0, a, 0, row, t);
+            wide_load<K3>(a1, a + s.a_ps, 0, row, t);
+            wide_load<K3>(b0, b, 0, row, t);
+            wide_load<K3>(b1, b + s.b_ps, 0, row, t);
+            wide_from_residues(a0); wide_from_residues(a1); wide_from_residues(b0); wide_from_residues(b1);
+#pragma unroll
+            for (int r = 0; r < 4; r++) {
+                x[r] += fp_mulmod(a0[r], b0[r], q.p, q.pinv);
+                y[r] += fp_mulmod(a0[r], b1[r], q.p, q.pinv) + fp_mulmod(a1[r], b0[r], q.p, q.pinv);
+            }
+        }
+        if (k & 1) {
+#pragma unroll
+            for (int r = 0; r < 4; r++) { x[r] = fp_norm(x[r], q.p, q.pinv); y[r] = fp_norm(y[r], q.p, q.pinv); }
+        }
+    }
+    if (!ROTATED && g.scaled) {
+        const double f = g.factor_ab.v[limb];
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+            x[r] = fp_mulmod(fp_norm(x[r], q.p, q.pinv), f, q.p, q.pinv);
+            y[r] = fp_mulmod(fp_norm(y[r], q.p, q.pinv), f, q.p, q.pinv);
+        }
+    }
+    if (s.add && (ROTATED || !u)) {
+        const double f = g.factor.v[limb];
+        wide_from_residues(c);
+#pragma unroll
+        for (int r = 0; r < 4; r++) x[r] += fp_mulmod(c[r], f, q.p, q.pinv);
+        if (!ROTATED) {
+            wide_from_residues(d);
+#pragma unroll
+            for (int r = 0; r < 4; r++) y[r] += fp_mulmod(d[r], f, q.p, q.pinv);
+        }
+    }
+    // x: no key needed (polynomial u, or the first); y: to be switched (or the second)
+    u64* out = g.out + (u64)entry * (ROTATED ? 2 : 3) * lw + limb_at + row * 1024u;
+    if (ROTATED || !u) wide_store_residues(make_rsrc(out + (ROTATED ? u : 0) * lw, 8192u), t, x, q);
+    u64* to = ROTATED ? g.pairs + ((u64)entry * 2 + u) * lw + limb_at + row * 1024u : out + (u ? 2 : 1) * lw;
+    const rsrc_t yr = make_rsrc(to, 8192u);
+    double v[4];
+#pragma unroll
+    for (int r = 0; r < 4; r++) {
+        v[r] = fp_norm(y[r], q.p, q.pinv);
+        v[r] = v[r] < 0.0 ? v[r] + q.p : v[r];
+        y[r] = __longlong_as_double((long long)fp_to_u64(v[r]));
+    }
+    wide_store(yr, t, y);
+    if (!transforms) {
+        wide_no_row();
+        return;
+    }
+    wide_inverse(v, 1.0f, w, lds_all + u * WIDE_LDS, t, q);
+    const rsrc_t mid = make_rsrc(g.mid + (ROTATED ? (u64)entry * 2 + u : (u64)entry) * lw + limb_at + row * 1024u, 8192u);
+#pragma unroll
+    for (int r = 0; r < 4; r++) bstoref(mid, t * 8u, (uint32_t)r * 2048u, v[r]);
+}
+
+hipError_t launch_product_rows_fp(const ProductArgs& g, int log_n, hipStream_t st) {
+    DRY_RUN_RETURN();
+    if (!g.fprimes || !g.out || !g.mid || !g.sinv || (g.galois && !g.pairs) || g.limbs < 1 || g.n_entries < 1 || g.n_first > (unsigned)g.n_entries ||
+        g.terms < 1 || (g.galois && g.scaled))
+        return hipErrorInvalidValue;
+    const u64 n = (u64)1 << log_n, tasks = ((u64)g.limbs * g.n_entries) << (log_n - 10);
+    if (log_n < 12 || log_n > 15 || tasks > 0x7fffff00u) return hipErrorInvalidValue;
+    for (int i = 0; i < 2; i++) {
+        const ProductSide& s = g.s[i];
+        if (i == 0 ? g.n_first == 0 : g.n_first == (unsigned)g.n_entries) continue;
+        if (!s.a || !s.b || s.a_div < 1 || s.a_ps < (u64)g.limbs * n || s.b_ps < (u64)g.limbs * n || (s.add && s.add_ps < (u64)g.limbs * n))
+            return hipErrorInvalidValue;
+    }
+    const dim3 grid((unsigned)((tasks + 7) / 8 * 8));
+    ProfScope prof__(g.galois ? "product_rows_kernel<true>" : "product_rows_kernel<false>", st);
+#define PRODUCT_CASE(K3)                                                                                                                  \
+    case 10 + K3:                                                                                                                         \
+        if (g.galois) hipLaunchKernelGGL((product_rows_kernel<K3, true>), grid, dim3(PRODUCT_NT), 0, st, g, (int)tasks);                  \
+        else hipLaunchKernelGGL((product_rows_kernel<K3, false>), grid, dim3(PRODUCT_NT), 0, st, g, (int)tasks);                          \
+        break;
+    switch (log_n) {
+        PRODUCT_CASE(2) PRODUCT_CASE(3) PRODUCT_CASE(4) PRODUCT_CASE(5)
+        default: return hipErrorInvalidValue;
+    }
+#undef PRODUCT_CASE
+    return hipGetLastError();
+}

@@ -1827,6 +1827,13 @@ static bool store_accumulators(const hisa_ctx* ctx, size_t entries, int ext_limb
     return entries * (size_t)ext_limbs * (ctx->N >> 10) < 1024;
 }
 
+// Of pairs: six digits are a longer chain of rounds, and memory stays ahead up to twice as many rows.  Scan of 100 tokens at N = 2^14, 12 limbs,
+// three ciphertexts (1024 rows, 960, ..) 679 -> 633 us, of 16384 at N = 2^15, 21 limbs (1792, 1728, ..) 1571 -> 1493; of twelve ciphertexts
+// there, 16 limbs (10560 ..) 2538 / 2547, four and two of 21 limbs (5376 ..) 2885 / 2891.
+static bool store_pair_accumulators(const hisa_ctx* ctx, size_t entries, int ext_limbs) {
+    return entries * (size_t)ext_limbs * (ctx->N >> 10) < 2048;
+}
+
 // C, D and E for n_steps rotations of the same B ciphertexts (entries rotation-major) whose digits are in x: a convolution's
 // taps rotate few ciphertexts many times, and a launch over B entries alone would leave most of the chip idle.
 // out: [n_steps][B] ciphertexts.
@@ -1910,8 +1917,23 @@ int product_keys_present(hisa_ctx* ctx, int32_t steps) {
     return HISA_OK;
 }
 
-int rotated_products_fp(hisa_ctx* ctx, const u64* pairs, const u64* plain, size_t n_pairs, int l, int32_t steps, u64* out) {
+// the products of g with what a key switch of theirs starts from: out and pairs as ProductArgs says, digits' columns in x
+static int product_digits_fp(hisa_ctx* ctx, ProductArgs& g, size_t n, const FpExt& x, u64* out, u64* pairs, ConvertArgs& c) {
+    g.out = out; g.pairs = pairs; g.mid = x.yp; g.n_entries = (int)n;
+    g.sinv = ctx->tabs.sinv; g.table_stride = split_table_words((int)ctx->log_n);
+    HIP_TRY(ctx, launch_product_rows_fp(g, (int)ctx->log_n, ctx->stream));
+    double *post_q, *post_p;
+    TRY(fp_post_tables(ctx, x.l, &post_q, &post_p, false));
+    c = convert_base(ctx, x.l, g.galois ? 2 * n : n);
+    TRY(modup_digits(ctx, c, x, false));
+    c.post = post_q;
+    HIP_TRY(ctx, launch_columns_fp(FP_FWD_CONV, c, ctx->stream));
+    return HISA_OK;
+}
+
+int rotated_products_fp(hisa_ctx* ctx, const ProductArgs& g_in, size_t n_pairs, int32_t steps, u64* out) {
     if (!fused_key_switch_available(ctx)) return fail(ctx, HISA_ERR_ARG, "no fused key-switch path for these parameters");
+    const int l = g_in.limbs;
     TRY(product_keys_present(ctx, steps));
     if (l < 2) return fail(ctx, HISA_ERR_DEPTH_EXHAUSTED, "no level to rescale into");
     if (t_analysis) {
@@ -1922,44 +1944,75 @@ int rotated_products_fp(hisa_ctx* ctx, const u64* pairs, const u64* plain, size_
         TALLY(key_switch_calls, HISA_OP_KEY_SWITCH_CALLS, 1, l);
         return HISA_OK;
     }
-    const u64 g = galois_of(ctx, steps);
-    const SwitchKey &key = ctx->keys.find(g)->second, &key2 = ctx->keys.find(product_key_id(g))->second;
-    const size_t n = ctx->N;
+    ProductArgs g = g_in;
+    g.galois = galois_of(ctx, steps);
+    const SwitchKey &key = ctx->keys.find(g.galois)->second, &key2 = ctx->keys.find(product_key_id(g.galois))->second;
+    const size_t n = ctx->N, lw = (size_t)l * n;
     const int K = (int)ctx->K, ext_limbs = l + K;
     FpExt x(ctx, 2 * n_pairs, l, K, (int)ctx->alpha);
-    if (!x.ok()) return HISA_ERR_OOM;
-    if (2 * x.digits <= FP_MAX_DIGITS) {      // five launches, as key_switch_fused_fp's
-        Division by;
-        TRY(division_by_p_and_last(ctx, l, &by));
-        const bool stored = store_accumulators(ctx, n_pairs, ext_limbs);
-        const size_t poly = n_pairs * 2 * n * sizeof(double);
-        Temp acc(ctx, poly * (size_t)by.n_acc, stored), down(ctx, poly * (size_t)(ext_limbs - by.n_acc));
-        if ((stored && !acc.ok()) || !down.ok()) return HISA_ERR_OOM;
-        double *post_q, *post_p;
-        TRY(fp_post_tables(ctx, l, &post_q, &post_p, false));
-        ConvertArgs c = convert_base(ctx, l, 2 * n_pairs);
-        TRY(modup_digits(ctx, c, x, false));
-        c.in = pairs; c.in_bs = (u64)l * n; c.post = post_q;
-        HIP_TRY(ctx, launch_inverse_rows_fp(c, ctx->stream));
-        HIP_TRY(ctx, launch_columns_fp(FP_FWD_CONV, c, ctx->stream));
-        c.n_entries = (unsigned)n_pairs; c.n_digits = 2 * x.digits; c.out_bs = 2 * x.ext_bs;
-        for (int d = 0; d < x.digits; d++) {
-            c.dg[x.digits + d] = c.dg[d];
-            c.dg[x.digits + d].out_pos0 += x.digits * ext_limbs;
-        }
-        InnerArgs g = {};
-        g.key = key.data; g.own = pairs; g.own_bs = (u64)2 * l * n;
-        g.add = plain; g.add_bs = (u64)2 * l * n; g.add_ps = (u64)l * n; g.add_polys = 2;
-        g.acc = stored ? acc.as<double>() : nullptr; g.down = down.as<double>();
-        const PairArgs second = {key2.data, (u64)l * n, x.digits};
-        return key_switch_divide_fp(ctx, c, g, by, nullptr, &second, l, n_pairs, out);
+    Temp plain(ctx, n_pairs * 2 * lw * sizeof(u64)), pairs(ctx, n_pairs * 2 * lw * sizeof(u64));
+    if (!x.ok() || !plain.ok() || !pairs.ok()) return HISA_ERR_OOM;
+    ConvertArgs c;
+    TRY(product_digits_fp(ctx, g, n_pairs, x, plain.u(), pairs.u(), c));
+    if (2 * x.digits > FP_MAX_DIGITS) {      // more digits than the rows of pairs count: inner products and division apart
+        Temp acc(ctx, n_pairs * 2 * (size_t)ext_limbs * n * sizeof(u64));
+        if (!acc.ok()) return HISA_ERR_OOM;
+        HIP_TRY(ctx, launch_forward_rows_fp(FP_FWD_CONV, c, ctx->stream));
+        HIP_TRY(ctx, launch_pair_inner_fp(ctx->tabs.fprimes, x.extp, x.digits, l, K, (int)ctx->L, (int)ctx->alpha, key.data, key2.data,
+                                          (int)ctx->total, pairs.u(), plain.u(), ctx->d_pmod, acc.u(), n_pairs, (int)ctx->log_n, ctx->stream));
+        return moddown_rescale_fp(ctx, acc.u(), n_pairs, l, nullptr, 0, 0, out);
     }
-    Temp acc(ctx, n_pairs * 2 * (size_t)ext_limbs * n * sizeof(u64));
-    if (!acc.ok()) return HISA_ERR_OOM;
-    TRY(key_switch_modup_fp(ctx, pairs, (u64)l * n, 2 * n_pairs, x));
-    HIP_TRY(ctx, launch_pair_inner_fp(ctx->tabs.fprimes, x.extp, x.digits, l, K, (int)ctx->L, (int)ctx->alpha, key.data, key2.data,
-                                      (int)ctx->total, pairs, plain, ctx->d_pmod, acc.u(), n_pairs, (int)ctx->log_n, ctx->stream));
-    return moddown_rescale_fp(ctx, acc.u(), n_pairs, l, nullptr, 0, 0, out);
+    Division by;
+    TRY(division_by_p_and_last(ctx, l, &by));
+    const bool stored = store_pair_accumulators(ctx, n_pairs, ext_limbs);
+    const size_t poly = n_pairs * 2 * n * sizeof(double);
+    Temp acc(ctx, poly * (size_t)by.n_acc, stored), down(ctx, poly * (size_t)(ext_limbs - by.n_acc));
+    if ((stored && !acc.ok()) || !down.ok()) return HISA_ERR_OOM;
+    c.n_entries = (unsigned)n_pairs; c.n_digits = 2 * x.digits; c.out_bs = 2 * x.ext_bs;
+    for (int d = 0; d < x.digits; d++) {
+        c.dg[x.digits + d] = c.dg[d];
+        c.dg[x.digits + d].out_pos0 += x.digits * ext_limbs;
+    }
+    InnerArgs r = {};
+    r.key = key.data; r.own = pairs.u(); r.own_bs = 2 * lw;
+    r.add = plain.u(); r.add_bs = 2 * lw; r.add_ps = lw; r.add_polys = 2;
+    r.acc = stored ? acc.as<double>() : nullptr; r.down = down.as<double>();
+    const PairArgs second = {key2.data, lw, x.digits};
+    return key_switch_divide_fp(ctx, c, r, by, nullptr, &second, l, n_pairs, out);
+}
+
+int products_rescale_fp(hisa_ctx* ctx, const ProductArgs& g_in, size_t n_cts, u64* out) {
+    if (!fused_key_switch_available(ctx)) return fail(ctx, HISA_ERR_ARG, "no fused key-switch path for these parameters");
+    const int l = g_in.limbs;
+    if (l < 2) return fail(ctx, HISA_ERR_DEPTH_EXHAUSTED, "no level to rescale into");
+    if (t_analysis) {
+        TALLY(mul, HISA_OP_MUL, n_cts, l);
+        TALLY(relinearize, HISA_OP_RELINEARIZE, n_cts, l);
+        TALLY(rescale, HISA_OP_RESCALE, n_cts, l);
+        TALLY(key_switch_calls, HISA_OP_KEY_SWITCH_CALLS, 1, l);
+        return HISA_OK;
+    }
+    auto it = ctx->keys.find(0);
+    if (it == ctx->keys.end()) return fail(ctx, HISA_ERR_NO_KEY, "no relinearisation key: call hisa_keygen");
+    ProductArgs g = g_in;
+    const size_t n = ctx->N, lw = (size_t)l * n;
+    const int ext_limbs = l + (int)ctx->K;
+    FpExt x(ctx, n_cts, l, (int)ctx->K, (int)ctx->alpha);
+    Temp three(ctx, n_cts * 3 * lw * sizeof(u64));
+    if (!x.ok() || !three.ok()) return HISA_ERR_OOM;
+    ConvertArgs c;
+    TRY(product_digits_fp(ctx, g, n_cts, x, three.u(), nullptr, c));
+    Division by;
+    TRY(division_by_p_and_last(ctx, l, &by));
+    const bool stored = store_accumulators(ctx, n_cts, ext_limbs);
+    const size_t poly = n_cts * 2 * n * sizeof(double);
+    Temp acc(ctx, poly * (size_t)by.n_acc, stored), down(ctx, poly * (size_t)(ext_limbs - by.n_acc));
+    if ((stored && !acc.ok()) || !down.ok()) return HISA_ERR_OOM;
+    InnerArgs r = {};
+    r.key = it->second.data; r.own = three.u() + 2 * lw; r.own_bs = 3 * lw;
+    r.add = three.u(); r.add_bs = 3 * lw; r.add_ps = lw; r.add_polys = 2;
+    r.acc = stored ? acc.as<double>() : nullptr; r.down = down.as<double>();
+    return key_switch_divide_fp(ctx, c, r, by, nullptr, nullptr, l, n_cts, out);
 }
 
 static int key_switch_core(hisa_ctx* ctx, const u64* d, u64 d_bs, u64 galois, size_t B, int l, const SwitchKey& key, const u64* add,

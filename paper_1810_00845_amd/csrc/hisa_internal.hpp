@@ -268,9 +268,35 @@ inline u64 product_key_id(u64 galois) { return ((u64)1 << 32) | galois; }
 u64 galois_of(const hisa_ctx* ctx, int32_t steps);   // 0: a multiple of the slots
 // HISA_ERR_NO_KEY unless both keys of the amount are there (a dry run notes the amount instead)
 int product_keys_present(hisa_ctx* ctx, int32_t steps);
-// a sigma(b) from its four products: pairs [n][2][l][N] holds a0 sigma(b1) and a1 sigma(b1), plain [n][2][l][N] a0 sigma(b0) and
-// a1 sigma(b0) with whatever else is to be added; out [n][2][l - 1][N] = (plain + both key switches) / q_{l-1}, one division
-int rotated_products_fp(hisa_ctx* ctx, const u64* pairs, const u64* plain, size_t n, int l, int32_t steps, u64* out);
+// Products of ciphertexts and what is added to them, on `limbs` limbs (operands of a higher level need no copy: ps apart are their
+// polynomials, bs their entries):  entry e: factor_ab a b + factor add,  a's entry e / a_div.  Entries from n_first on take
+// their operands from s[1].  terms > 1 (entries of s[0], a_div 1): the sum over entries e terms .. of a and of b.
+struct LimbFactors { double v[HISA_MAX_PRIMES]; };       // residues modulo q_i, centred
+struct ProductSide {
+    const u64 *a, *b, *add;
+    u64 a_bs, a_ps, b_bs, b_ps, add_bs, add_ps;
+    unsigned a_div;
+};
+struct ProductArgs {
+    const FpPrime* fprimes;
+    ProductSide s[2];
+    unsigned n_first, terms;
+    int limbs, scaled;                   // scaled: by factor_ab (products without a rotation)
+    u64 galois;                          // of b; 0: none
+    LimbFactors factor, factor_ab;
+    // set by whoever switches keys: the polynomials that need no key ([n][2][limbs][N], or the first two of [n][3][limbs][N]), those that
+    // do ([n][2][limbs][N]: a0 sigma(b1), a1 sigma(b1); or the third of [n][3][limbs][N]: a1 b1), and the latter after the inverse rows
+    u64 *out, *pairs;
+    double* mid;
+    const double* sinv;
+    u64 table_stride;
+    int n_entries;
+};
+hipError_t launch_product_rows_fp(const ProductArgs& g, int log_n, hipStream_t st);
+// out [n][2][limbs - 1][N] = the products of g / q_{limbs - 1}: with b rotated by `steps`, or relinearised (products_rescale_fp);
+// key switches and rescale are one division
+int rotated_products_fp(hisa_ctx* ctx, const ProductArgs& g, size_t n, int32_t steps, u64* out);
+int products_rescale_fp(hisa_ctx* ctx, const ProductArgs& g, size_t n, u64* out);
 // three-polynomial ciphertexts -> two polynomials at the same level: [n][3][l][N] -> out [n][2][l][N]
 int relinearize_fp(hisa_ctx* ctx, const u64* cts3, size_t n, int l, u64* out);
 int rescale_fp(hisa_ctx* ctx, const u64* in, size_t n_polys, int l, u64* out);   // [n_polys][l][N] -> [n_polys][l - 1][N]

@@ -11,7 +11,6 @@
 
 #define NT 256
 
-struct LimbFactors { double v[HISA_MAX_PRIMES]; };       // residues modulo q_i, centred
 static LimbFactors limb_factors(const hisa_ctx* ctx, double value, int limbs) {
     LimbFactors f = {};
     for (int i = 0; i < limbs; i++) {
@@ -19,105 +18,6 @@ static LimbFactors limb_factors(const hisa_ctx* ctx, double value, int limbs) {
         f.v[i] = r > q / 2 ? -(double)(q - r) : (double)r;
     }
     return f;
-}
-
-// ---------------------------------------------------------------------------
-// products of ciphertexts
-// ---------------------------------------------------------------------------
-// Entry e of out: factor_ab a b (+ factor add), before key switching.  Operands are ciphertexts [2][..][N] with polynomials `ps` and
-// entries `bs` words apart, of which the first `limbs` limbs are read: a of a higher level needs no copy to be used lower.
-// Two groups of entries in one launch: those from n_first on take their operands from s[1].
-//   ROTATED: b is read through sigma_g; out holds (a0 b0 + f c0, a1 b0 + f c1) per entry, pairs (a0 b1, a1 b1)
-//   else:    out [3]: a0 b0 + f c0, a0 b1 + a1 b0 + f c1, a1 b1
-// terms > 1 (group 0 only): entry e is the sum over entries e terms .. of both operands.
-// Bound by memory.  Values: canonical residues in, products within 0.875 p, sums normalised before they pass 2^52.
-struct ProductSide {
-    const u64 *a, *b, *add;
-    u64 a_bs, a_ps, b_bs, b_ps, add_bs, add_ps;
-    unsigned a_div;                  // entry e multiplies a's entry e / a_div
-};
-struct ProductArgs {
-    const FpPrime* fprimes;
-    ProductSide s[2];
-    unsigned n_first, terms;
-    int limbs, scaled;               // scaled: by factor_ab (not ROTATED)
-    u64 galois;
-    u64 *out, *pairs;
-    LimbFactors factor, factor_ab;
-};
-
-__device__ __forceinline__ double product_centred(u64 x, double p, double half) { return fp_centred_from_u64(x, p, half); }
-
-template <bool ROTATED>
-__global__ __launch_bounds__(NT) void ciphertext_product_kernel(ProductArgs g, int log_n) {
-    const u64 n = (u64)1 << log_n;
-    const int limb = blockIdx.y;
-    const unsigned entry = blockIdx.z, side = entry >= g.n_first ? 1 : 0, e = side ? entry - g.n_first : entry;
-    const ProductSide& s = g.s[side];
-    const double p = as_const(&g.fprimes[limb].p)[0], pinv = as_const(&g.fprimes[limb].p)[1], half = as_const(&g.fprimes[limb].p)[2];
-    const uint32_t j = blockIdx.x * NT + threadIdx.x;
-    const u64 at = (u64)limb * n + j, bt = (u64)limb * n + (ROTATED ? galois_src_fp(j, g.galois, log_n) : j);
-    double v[4] = {0.0, 0.0, 0.0, 0.0};
-    const unsigned terms = side ? 1 : g.terms;
-    for (unsigned t = 0; t < terms; t++) {
-        const u64* a = s.a + (u64)(terms > 1 ? e * terms + t : e / s.a_div) * s.a_bs + at;
-        const u64* b = s.b + (u64)(e * terms + t) * s.b_bs + bt;
-        const double a0 = product_centred(a[0], p, half), a1 = product_centred(a[s.a_ps], p, half);
-        const double b0 = product_centred(b[0], p, half), b1 = product_centred(b[s.b_ps], p, half);
-        v[0] += fp_mulmod(a0, b0, p, pinv);
-        v[1] += fp_mulmod(a1, b0, p, pinv);
-        v[2] += fp_mulmod(a0, b1, p, pinv);
-        v[3] += fp_mulmod(a1, b1, p, pinv);
-        if ((t & 3) == 3) {
-#pragma unroll
-            for (int k = 0; k < 4; k++) v[k] = fp_norm(v[k], p, pinv);
-        }
-    }
-    if (!ROTATED) v[1] += v[2];
-    if (!ROTATED && g.scaled) {
-        const double f = g.factor_ab.v[limb];
-#pragma unroll
-        for (int k = 0; k < 4; k++)
-            if (k != 2) v[k] = fp_mulmod(fp_norm(v[k], p, pinv), f, p, pinv);
-    }
-    if (s.add) {
-        const u64* c = s.add + (u64)e * s.add_bs + at;
-        const double f = g.factor.v[limb];
-        v[0] += fp_mulmod(product_centred(c[0], p, half), f, p, pinv);
-        v[1] += fp_mulmod(product_centred(c[s.add_ps], p, half), f, p, pinv);
-    }
-    const u64 lw = (u64)g.limbs * n;
-    if (ROTATED) {
-        u64 *plain = g.out + (u64)entry * 2 * lw + at, *pair = g.pairs + (u64)entry * 2 * lw + at;
-        plain[0] = fp_canonical(v[0], p, pinv);
-        plain[lw] = fp_canonical(v[1], p, pinv);
-        pair[0] = fp_canonical(v[2], p, pinv);
-        pair[lw] = fp_canonical(v[3], p, pinv);
-    } else {
-        u64* out = g.out + (u64)entry * 3 * lw + at;
-        out[0] = fp_canonical(v[0], p, pinv);
-        out[lw] = fp_canonical(v[1], p, pinv);
-        out[2 * lw] = fp_canonical(v[3], p, pinv);
-    }
-}
-
-static hipError_t launch_products(const ProductArgs& g, bool rotated, unsigned entries, int log_n, hipStream_t st) {
-    DRY_RUN_RETURN();
-    if (!g.fprimes || !g.out || (rotated && (!g.pairs || !g.galois)) || g.limbs < 1 || entries == 0 || entries > 65535 || g.n_first > entries ||
-        g.terms < 1)
-        return hipErrorInvalidValue;
-    const u64 n = (u64)1 << log_n;
-    for (int i = 0; i < 2; i++) {
-        const ProductSide& s = g.s[i];
-        if (i == 0 ? g.n_first == 0 : g.n_first == entries) continue;
-        if (!s.a || !s.b || s.a_div < 1 || s.a_ps < (u64)g.limbs * n || s.b_ps < (u64)g.limbs * n || (s.add && s.add_ps < (u64)g.limbs * n))
-            return hipErrorInvalidValue;
-    }
-    const dim3 grid((unsigned)(n / NT), g.limbs, entries);
-    ProfScope prof__(rotated ? "ciphertext_product_kernel<true>" : "ciphertext_product_kernel<false>", st);
-    if (rotated) hipLaunchKernelGGL(ciphertext_product_kernel<true>, grid, dim3(NT), 0, st, g, log_n);
-    else hipLaunchKernelGGL(ciphertext_product_kernel<false>, grid, dim3(NT), 0, st, g, log_n);
-    return hipGetLastError();
 }
 
 // ---------------------------------------------------------------------------
@@ -266,28 +166,16 @@ static int rotated_products(hisa_ctx* ctx, const ProductArgs& g, size_t entries,
     const size_t unit = std::max(g.s[0].a_div, 1u);
     if (part < entries && part > unit) part -= part % unit;
     if (part < entries && (part % unit || g.n_first % unit)) part = 1;
-    Temp plain(ctx, part * 2 * lw * sizeof(u64)), pairs(ctx, part * 2 * lw * sizeof(u64));
-    if (!plain.ok() || !pairs.ok()) return HISA_ERR_OOM;
     for (size_t e0 = 0; e0 < entries; e0 += part) {
         const unsigned cnt = (unsigned)std::min(part, entries - e0);
-        ProductArgs p = product_part(g, (unsigned)e0, cnt);
-        p.galois = galois_of(ctx, step);
-        p.out = plain.u(); p.pairs = pairs.u();
-        HIP_TRY(ctx, launch_products(p, true, cnt, (int)ctx->log_n, ctx->stream));
-        TRY(rotated_products_fp(ctx, pairs.u(), plain.u(), cnt, g.limbs, step, out + e0 * 2 * (lw - n)));
+        TRY(rotated_products_fp(ctx, product_part(g, (unsigned)e0, cnt), cnt, step, out + e0 * 2 * (lw - n)));
     }
     return HISA_OK;
 }
 // products without a rotation, relinearised and rescaled: out [entries][2][l - 1][N]
-static int relinearised_products(hisa_ctx* ctx, ProductArgs g, size_t entries, u64* out) {
-    const size_t n = ctx->N, lw = (size_t)g.limbs * n;
+static int relinearised_products(hisa_ctx* ctx, const ProductArgs& g, size_t entries, u64* out) {
     if (entries > 16384) return fail(ctx, HISA_ERR_ARG, "%zu ciphertexts in one call", entries);
-    if (t_analysis) TALLY(mul, HISA_OP_MUL, entries, g.limbs);
-    Temp three(ctx, entries * 3 * lw * sizeof(u64));
-    if (!three.ok()) return HISA_ERR_OOM;
-    g.out = three.u();
-    HIP_TRY(ctx, launch_products(g, false, (unsigned)entries, (int)ctx->log_n, ctx->stream));
-    return relinearize_rescale_fp(ctx, three.u(), 3 * lw, entries, g.limbs, out);
+    return products_rescale_fp(ctx, g, entries, out);
 }
 
 // Nothing throws across the C boundary: what the host containers may throw becomes an error code.
