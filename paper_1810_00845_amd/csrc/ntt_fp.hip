@@ -557,6 +557,154 @@ __device__ __forceinline__ void inner_product_sum(
     }
 }
 
+struct SumArgs {
+    const FpPrime* fprimes;
+    const double* ext;
+    u64 ext_bs;
+    int l, K, L, alpha, n_steps, total, log_n;
+    uint32_t n_batch, groups;
+    const u64 *own_src, *c0_src, *plain, *pmod;
+    u64 own_bs, plain_bs, acc_bs;
+    u64* acc;
+    IpSteps steps;
+};
+template <bool ONCE>
+__device__ __forceinline__ void key_load2(rsrc_t r, uint32_t lane_off, uint32_t row_off, double (&v)[2]) {
+    if (!ONCE) return bload2(r, lane_off, row_off, v[0], v[1]);
+    const u32x4_t d = __builtin_amdgcn_raw_buffer_load_b128(r, (int)lane_off, (int)row_off, NONTEMPORAL);
+    v[0] = mk64(d.x, d.y);
+    v[1] = mk64(d.z, d.w);
+}
+
+// The same for rotations of one ciphertext per output, where a launch fills the chip.  A wave of the kernel above spends half of its
+// instructions on 64-bit addresses and on choosing between own and extended digits, and asks for 512 bytes at a time.  Here rows are
+// buffer resources (the lane's offset changes once a rotation, the row's is scalar), what differs for a limb's own digit is a
+// uniform branch, and a thread owns two neighbouring coefficients, which an automorphism leaves neighbours.  An XCD keeps to one half of
+// a limb at a time -- an automorphism moves no value across the halves -- with the groups of outputs of a block next to each other.
+// Seven rotations of eight outputs at N = 2^15, 28 limbs 221 -> 191 us (a coefficient a thread 206): 36 to 40 million vector instructions for
+// 56, and 6.4 TB/s of what the L2 passes on (keys 308 MB, digits 172 MB, each group of four outputs its own).  Whole sums, us, as
+// above / here: of four outputs at N = 2^15, 21 limbs, 3, 7 and 15 rotations 225, 286, 422 / 217, 273, 379 (keys past the caches: 207, 256,
+// 346), of twelve 531, 721, 1130 / 524, 645, 910; at N = 2^14, 12 limbs eight 116, 151, 229 / 113, 134, 188; of two 139, 180, 268 / 136, 185,
+// 268 and of one 134 / 150 (seven): those stay above.
+#define HALVES_NT 256
+template <int DIGITS, bool ONCE>
+__global__ __launch_bounds__(HALVES_NT, 2) void inner_product_sum_halves_kernel(SumArgs g) {
+    const u64 n = (u64)1 << g.log_n;
+    const uint32_t blocks = (uint32_t)n / 4 / HALVES_NT, per = blocks * g.groups, local = blockIdx.x >> 3;
+    const uint32_t unit = (blockIdx.x & 7) + 8 * (local / per), at = local % per;
+    const int x = (int)(unit >> 1), ext_limbs = g.l + g.K;
+    if (x >= ext_limbs) return;
+    const uint32_t j = ((at / g.groups + (unit & 1) * blocks) * HALVES_NT + threadIdx.x) * 2;
+    const uint32_t b0 = (at % g.groups) * IPS_BCH;
+    const int live = (int)(g.n_batch - b0 < IPS_BCH ? g.n_batch - b0 : IPS_BCH);
+    const int prime = x < g.l ? x : g.L + (x - g.l), own = x < g.l ? x / g.alpha : -1;
+    const double p = as_const(&g.fprimes[prime].p)[0], pinv = as_const(&g.fprimes[prime].p)[1];
+    const FpSumPlan plan = fp_sum_plan(p);
+    const int fold_every = plan.terms / DIGITS;
+    const uint32_t row = (uint32_t)(n * 8), ext_u = (uint32_t)(g.ext_bs * 8), own_u = (uint32_t)(g.own_bs * 8);
+    const rsrc_t ext_r = make_rsrc(g.ext + b0 * g.ext_bs + (u64)x * n, (uint32_t)(live - 1) * ext_u + (uint32_t)((DIGITS - 1) * ext_limbs + 1) * row);
+    const rsrc_t own_r = make_rsrc(g.own_src + b0 * g.own_bs + (u64)(x < g.l ? x : 0) * n, (uint32_t)(live - 1) * own_u + row);
+    const rsrc_t c0_r = make_rsrc(g.c0_src + b0 * g.own_bs + (u64)(x < g.l ? x : 0) * n, (uint32_t)(live - 1) * own_u + row);
+    FpSum sb[IPS_BCH][2], sa[IPS_BCH][2];
+    double tc[IPS_BCH][2];
+#pragma unroll
+    for (int u = 0; u < IPS_BCH; u++)
+#pragma unroll
+        for (int i = 0; i < 2; i++) { sb[u][i] = sa[u][i] = FpSum{plan.base, 0.0}; tc[u][i] = 0.0; }
+    auto fold = [&](FpSum& s) { s = FpSum{plan.base, fp_norm(fp_sum_value(s, plan.base, p, pinv), p, pinv)}; };
+    int pending = 0, c0_pending = 0;
+    const uint32_t key_bytes = (uint32_t)(2 * DIGITS * g.total) * row;
+    for (int s = 0; s < g.n_steps; s++) {
+        const rsrc_t key_r = make_rsrc((const double*)g.steps.key[s] + (u64)prime * n, key_bytes - (uint32_t)prime * row);
+        const uint32_t from = galois_src_fp(j, g.steps.galois[s], g.log_n);
+        const uint32_t src = (from & ~1u) * 8u;      // neighbours come from a pair of neighbours, in either order
+        const bool turned = from & 1;
+        double kb[DIGITS][2], ka[DIGITS][2], e[DIGITS][IPS_BCH][2], c0[IPS_BCH][2];
+#pragma unroll
+        for (int d = 0; d < DIGITS; d++) {
+            key_load2<ONCE>(key_r, j * 8u, (uint32_t)(2 * d * g.total) * row, kb[d]);
+            key_load2<ONCE>(key_r, j * 8u, (uint32_t)((2 * d + 1) * g.total) * row, ka[d]);
+        }
+#pragma unroll
+        for (int d = 0; d < DIGITS; d++) {
+            if (d == own) {
+#pragma unroll
+                for (int u = 0; u < IPS_BCH; u++) bload2(own_r, src, (uint32_t)u * own_u, e[d][u][0], e[d][u][1]);      // beyond the last output: zero
+            } else {
+#pragma unroll
+                for (int u = 0; u < IPS_BCH; u++) bload2(ext_r, src, (uint32_t)u * ext_u + (uint32_t)(d * ext_limbs) * row, e[d][u][0], e[d][u][1]);
+            }
+        }
+        if (x < g.l) {
+#pragma unroll
+            for (int u = 0; u < IPS_BCH; u++) bload2(c0_r, src, (uint32_t)u * own_u, c0[u][0], c0[u][1]);
+        }
+#pragma unroll
+        for (int d = 0; d < DIGITS; d++) {
+            if (d == own) {
+#pragma unroll
+                for (int u = 0; u < IPS_BCH; u++)
+#pragma unroll
+                    for (int i = 0; i < 2; i++) e[d][u][i] = fp_norm(fp_from_u64((u64)__double_as_longlong(e[d][u][i])), p, pinv);
+            }
+#pragma unroll
+            for (int u = 0; u < IPS_BCH; u++) {
+                const double e0 = turned ? e[d][u][1] : e[d][u][0], e1 = turned ? e[d][u][0] : e[d][u][1];
+                fp_sum_add(sb[u][0], e0, kb[d][0]);
+                fp_sum_add(sa[u][0], e0, ka[d][0]);
+                fp_sum_add(sb[u][1], e1, kb[d][1]);
+                fp_sum_add(sa[u][1], e1, ka[d][1]);
+            }
+        }
+        if (x < g.l) {
+            c0_pending++;
+#pragma unroll
+            for (int u = 0; u < IPS_BCH; u++) {
+                tc[u][0] += fp_from_u64((u64)__double_as_longlong(turned ? c0[u][1] : c0[u][0]));
+                tc[u][1] += fp_from_u64((u64)__double_as_longlong(turned ? c0[u][0] : c0[u][1]));
+            }
+            if (c0_pending == 6) {
+                c0_pending = 0;
+#pragma unroll
+                for (int u = 0; u < IPS_BCH; u++)
+#pragma unroll
+                    for (int i = 0; i < 2; i++) tc[u][i] = fp_norm(tc[u][i], p, pinv);
+            }
+        }
+        if (++pending == fold_every) {
+            pending = 0;
+#pragma unroll
+            for (int u = 0; u < IPS_BCH; u++)
+#pragma unroll
+                for (int i = 0; i < 2; i++) { fold(sb[u][i]); fold(sa[u][i]); }
+        }
+    }
+    const double pm = x < g.l ? fp_from_u64(g.pmod[prime]) : 0.0;
+#pragma unroll
+    for (int u = 0; u < IPS_BCH; u++) {
+        if (u >= live) break;
+        u64 vb[2], va[2];
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            fold(sb[u][i]); fold(sa[u][i]);
+            double b = sb[u][i].l, a = sa[u][i].l, c = fp_norm(tc[u][i], p, pinv);
+            if (x < g.l) {
+                if (g.plain) {
+                    const u64* add = g.plain + (b0 + u) * g.plain_bs + (u64)x * n + j + i;
+                    c += fp_from_u64(add[0]);
+                    a += fp_mulmod(fp_from_u64(add[(u64)g.l * n]), pm, p, pinv);
+                }
+                b += fp_mulmod(c, pm, p, pinv);
+            }
+            vb[i] = fp_canonical(b, p, pinv);
+            va[i] = fp_canonical(a, p, pinv);
+        }
+        const rsrc_t to = make_rsrc(g.acc + (b0 + u) * g.acc_bs + (u64)x * n, (uint32_t)(ext_limbs + 1) * row);
+        bstore2(to, j * 8u, 0, vb[0], vb[1]);
+        bstore2(to, j * 8u, (uint32_t)ext_limbs * row, va[0], va[1]);
+    }
+}
+
 #define SUM_PARAMS                                                                                                                        \
     const FpPrime *fprimes, const double *ext, u64 ext_bs, int digits, int l, int K, int L, int alpha, IpSteps steps, int n_steps, int total, \
         const u64 *own_src, u64 own_bs, u64 *acc, u64 acc_bs, u64 n_batch, int shared_input, const u64 *c0_src, const u64 *plain,         \
@@ -592,6 +740,21 @@ hipError_t launch_inner_product_sum_fp(const FpPrime* fprimes, const double* ext
     const bool few = ((u64)groups_of_outputs * (l + K) << log_n) / IPF_NT < IPS_FEW;
     dim3 grid((1u << log_n) / (few ? 64 : IPF_NT), groups_of_outputs, l + K);
     const bool once = groups_of_outputs == 1 && ((u64)n_steps * digits * 2 * (l + K) << (log_n + 3)) > STREAMED_KEY_BYTES;
+    // rotations of three outputs and more, up to three digits known to the compiler, offsets that fit a buffer resource
+    if (shared_input && n_batch > 2 && !few && digits < 4 && IPS_BCH * ext_bs * 8 <= 0x7fffffffu && ((u64)2 * digits * total << (log_n + 3)) <= 0x7fffffffu) {
+        SumArgs g = {fprimes, ext, ext_bs, l, K, L, alpha, n_steps, total, log_n, (uint32_t)n_batch, groups_of_outputs, own_src, c0_src, plain, pmod,
+                     own_bs, plain_bs, acc_bs, acc, steps};
+        const dim3 units(8 * ((2 * (l + K) + 7) / 8) * groups_of_outputs * (unsigned)(n / 4 / HALVES_NT));
+        ProfScope prof__("inner_product_sum_halves_kernel", st);
+#define HALVES_LAUNCH(D)                                                                                                 \
+    if (once) hipLaunchKernelGGL((inner_product_sum_halves_kernel<D, true>), units, dim3(HALVES_NT), 0, st, g);          \
+    else hipLaunchKernelGGL((inner_product_sum_halves_kernel<D, false>), units, dim3(HALVES_NT), 0, st, g);                 \
+    return hipGetLastError()
+        if (digits == 1) { HALVES_LAUNCH(1); }
+        if (digits == 2) { HALVES_LAUNCH(2); }
+        HALVES_LAUNCH(3);
+#undef HALVES_LAUNCH
+    }
     ProfScope prof__(once ? "inner_product_sum_once_kernel" : "inner_product_sum_fp_kernel", st);
 #define SUM_LAUNCH(G, D)                                                                                                \
     if (once) hipLaunchKernelGGL((inner_product_sum_once_kernel<G, D>), grid, dim3(IPF_NT), 0, st, SUM_ARGS);            \
