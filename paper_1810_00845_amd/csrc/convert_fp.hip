@@ -1789,7 +1789,7 @@ __global__ __launch_bounds__(PRODUCT_NT, 4) void product_rows_kernel(ProductArgs
         }
     }
     if (!ROTATED && g.scaled) {
-        const double f = g.factor_ab.v[limb];
+        const double f = fp_whole(g.factor_ab, q.p, q.pinv);
 #pragma unroll
         for (int r = 0; r < 4; r++) {
             x[r] = fp_mulmod(fp_norm(x[r], q.p, q.pinv), f, q.p, q.pinv);
@@ -1797,7 +1797,7 @@ __global__ __launch_bounds__(PRODUCT_NT, 4) void product_rows_kernel(ProductArgs
         }
     }
     if (s.add && (ROTATED || !u)) {
-        const double f = g.factor.v[limb];
+        const double f = fp_whole(g.factor, q.p, q.pinv);
         wide_from_residues(c);
 #pragma unroll
         for (int r = 0; r < 4; r++) x[r] += fp_mulmod(c[r], f, q.p, q.pinv);

@@ -88,6 +88,21 @@ FP_HD uint64_t fp_to_u64(double v) {
     return c.u & 0x000FFFFFFFFFFFFFULL;
 }
 
+// a whole number of magnitude below 2^120 held in a double -> |result| <= p/2 (1 + 2^-48)
+FP_HD double fp_whole(double v, double p, double pinv) {
+    union { double d; uint64_t u; } c;
+    c.d = v;
+    int e = (int)((c.u >> 52) & 0x7ff) - 1075;              // v = m 2^e, |m| in [2^52, 2^53)
+    if (e <= 0) return fp_norm(v, p, pinv);                 // below 2^53
+    c.u -= (uint64_t)e << 52;
+    double r = fp_norm(c.d, p, pinv);
+    for (; e > 0; e -= 40) {
+        c.u = (uint64_t)(1023 + (e < 40 ? e : 40)) << 52;
+        r = fp_mulmod(r, fp_norm(c.d, p, pinv), p, pinv);
+    }
+    return fp_norm(r, p, pinv);
+}
+
 // any lazy value -> canonical residue in [0, p)
 FP_HD uint64_t fp_canonical(double v, double p, double pinv) {
     double r = fp_norm(v, p, pinv);

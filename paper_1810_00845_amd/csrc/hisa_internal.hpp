@@ -271,7 +271,6 @@ int product_keys_present(hisa_ctx* ctx, int32_t steps);
 // Products of ciphertexts and what is added to them, on `limbs` limbs (operands of a higher level need no copy: ps apart are their
 // polynomials, bs their entries):  entry e: factor_ab a b + factor add,  a's entry e / a_div.  Entries from n_first on take
 // their operands from s[1].  terms > 1 (entries of s[0], a_div 1): the sum over entries e terms .. of a and of b.
-struct LimbFactors { double v[HISA_MAX_PRIMES]; };       // residues modulo q_i, centred
 struct ProductSide {
     const u64 *a, *b, *add;
     u64 a_bs, a_ps, b_bs, b_ps, add_bs, add_ps;
@@ -283,7 +282,7 @@ struct ProductArgs {
     unsigned n_first, terms;
     int limbs, scaled;                   // scaled: by factor_ab (products without a rotation)
     u64 galois;                          // of b; 0: none
-    LimbFactors factor, factor_ab;
+    double factor, factor_ab;            // whole numbers below 2^120
     // set by whoever switches keys: the polynomials that need no key ([n][2][limbs][N], or the first two of [n][3][limbs][N]), those that
     // do ([n][2][limbs][N]: a0 sigma(b1), a1 sigma(b1); or the third of [n][3][limbs][N]: a1 b1), and the latter after the inverse rows
     u64 *out, *pairs;

@@ -11,15 +11,6 @@
 
 #define NT 256
 
-static LimbFactors limb_factors(const hisa_ctx* ctx, double value, int limbs) {
-    LimbFactors f = {};
-    for (int i = 0; i < limbs; i++) {
-        const u64 q = ctx->mod[i], r = double_to_residue(value, q);
-        f.v[i] = r > q / 2 ? -(double)(q - r) : (double)r;
-    }
-    return f;
-}
-
 // ---------------------------------------------------------------------------
 // the inner products of a pair with its two keys
 // ---------------------------------------------------------------------------
@@ -236,7 +227,7 @@ static int scan_run(hisa_ctx* ctx, Cts gates, double gate_scale, Cts x, size_t n
         ProductArgs g = product_base(ctx, l);
         double factor;
         TRY(whole_factor(ctx, gate_scale, &factor));
-        g.factor = limb_factors(ctx, factor, l);
+        g.factor = factor;
         g.n_first = (unsigned)n_x;
         operand_a(g.s[0], gates, n, shared); operand_b(g.s[0], x, n); operand_add(g.s[0], x, n);
         operand_a(g.s[1], gates, n, 1); operand_b(g.s[1], gates, n);
@@ -349,7 +340,7 @@ static int recurrence_step(hisa_ctx* ctx, const hisa_tensor* gates, const hisa_t
     TRY(o.make(n_x, l - 1, sg * ss / (double)ctx->mod[l - 1]));
     ProductArgs g = product_base(ctx, l);
     g.n_first = (unsigned)n_x;
-    g.factor = limb_factors(ctx, factor, l);
+    g.factor = factor;
     operand_a(g.s[0], cts_of(gg.b, lg), n, shared);
     operand_b(g.s[0], cts_of(gs.b, ls), n);
     operand_add(g.s[0], cts_of(gx.b, lx), n);
@@ -490,23 +481,22 @@ __global__ __launch_bounds__(NT) void group_moments_kernel(const FpPrime* fprime
 }
 
 // k_w x and -k_y x side by side: the variances, polynomials [polys][limbs][N], on their way to two scales
-struct StartArgs { LimbFactors w, y; };
-__global__ __launch_bounds__(NT) void norm_times_kernel(const FpPrime* fprimes, const u64* x, u64* out, int limbs, StartArgs k, int log_n) {
+__global__ __launch_bounds__(NT) void norm_times_kernel(const FpPrime* fprimes, const u64* x, u64* out, int limbs, double kw, double ky, int log_n) {
     const int limb = blockIdx.y;
     const u64 at = (((u64)blockIdx.z * limbs + limb) << log_n) + (u64)blockIdx.x * NT + threadIdx.x;
     const double p = as_const(&fprimes[limb].p)[0], pinv = as_const(&fprimes[limb].p)[1], half = as_const(&fprimes[limb].p)[2];
     const double v = fp_centred_from_u64(x[at], p, half);
-    out[at] = fp_canonical(fp_mulmod(v, k.w.v[limb], p, pinv), p, pinv);
-    out[at + (((u64)gridDim.z * limbs) << log_n)] = fp_canonical(fp_mulmod(v, k.y.v[limb], p, pinv), p, pinv);
+    out[at] = fp_canonical(fp_mulmod(v, fp_whole(kw, p, pinv), p, pinv), p, pinv);
+    out[at + (((u64)gridDim.z * limbs) << log_n)] = fp_canonical(fp_mulmod(v, fp_whole(ky, p, pinv), p, pinv), p, pinv);
 }
 
 // The first polynomials of w and of y plus a constant each, in place (a constant polynomial is that constant at every evaluation point):
 // entries [2 groups], w in front
-__global__ __launch_bounds__(NT) void norm_start_kernel(const FpPrime* fprimes, u64* x, int limbs, StartArgs c, int log_n) {
+__global__ __launch_bounds__(NT) void norm_start_kernel(const FpPrime* fprimes, u64* x, int limbs, double cw, double cy, int log_n) {
     const int limb = blockIdx.y;
     const u64 at = (((u64)blockIdx.z * 2 * limbs + limb) << log_n) + (u64)blockIdx.x * NT + threadIdx.x;
     const double p = as_const(&fprimes[limb].p)[0], pinv = as_const(&fprimes[limb].p)[1];
-    x[at] = fp_canonical(fp_from_u64(x[at]) + (2 * blockIdx.z < gridDim.z ? c.w.v[limb] : c.y.v[limb]), p, pinv);
+    x[at] = fp_canonical(fp_from_u64(x[at]) + (2 * blockIdx.z < gridDim.z ? fp_whole(cw, p, pinv) : fp_whole(cy, p, pinv)), p, pinv);
 }
 
 // out = (n x - m) gamma: x entry e, m entry e / per, gamma plaintext e % images, on the first `limbs` limbs
@@ -517,14 +507,14 @@ struct CentreArgs {
     unsigned per, period;
     int limbs;
     u64* out;
-    LimbFactors count;
+    double count;
 };
 __global__ __launch_bounds__(NT) void norm_centre_kernel(CentreArgs g, int log_n) {
     const u64 n = (u64)1 << log_n, lw = (u64)g.limbs * n;
     const int limb = blockIdx.y;
     const u64 e = blockIdx.z, at = (u64)limb * n + (u64)blockIdx.x * NT + threadIdx.x;
     const double p = as_const(&g.fprimes[limb].p)[0], pinv = as_const(&g.fprimes[limb].p)[1], half = as_const(&g.fprimes[limb].p)[2];
-    const double w = fp_centred_from_u64(g.gamma[(e % g.period) * lw + at], p, half), count = g.count.v[limb];
+    const double w = fp_centred_from_u64(g.gamma[(e % g.period) * lw + at], p, half), count = fp_whole(g.count, p, pinv);
 #pragma unroll
     for (int poly = 0; poly < 2; poly++) {
         const double x = fp_centred_from_u64(g.x[e * g.x_bs + poly * g.x_ps + at], p, half);
@@ -595,6 +585,7 @@ static int norm_schedule(hisa_ctx* ctx, const hisa_norm_geom& geom, double n, in
     odd_cubic(a, b, &c1, &c3);
     r->kw = fmax(1.0, whole(s * NORM_SHARE * q(level) / sv));
     r->ky = fmax(1.0, whole(s * c3 * q(level) / sv));
+    if (!(r->kw < 0x1p120) || !(r->ky < 0x1p120)) return fail(ctx, HISA_ERR_SCALE_MISMATCH, "a variance of %g is too small for the scale", geom.var_hi);
     const double sw = sv * r->kw / q(level);
     double sy = sv * r->ky / q(level) / c3;
     level -= 1;
@@ -798,17 +789,16 @@ static int norm_apply(hisa_ctx* ctx, const hisa_tensor* in, const hisa_norm_plan
     {
         ProductArgs g = product_base(ctx, l);
         g.n_first = (unsigned)groups; g.scaled = 1;
-        g.factor_ab = limb_factors(ctx, -1.0, l);
-        g.factor = limb_factors(ctx, r.count, l);
+        g.factor_ab = -1.0;
+        g.factor = r.count;
         operand_a(g.s[0], total, n, 1); operand_b(g.s[0], total, n); operand_add(g.s[0], total2, n);
         TRY(relinearised_products(ctx, g, groups, v.u()));
         l -= 1;
     }
     if (t_analysis) TALLY(mul_scalar, HISA_OP_MUL_SCALAR, 2 * groups, l);
     if (!t_analysis) {
-        const StartArgs k = {limb_factors(ctx, r.kw, l), limb_factors(ctx, -r.ky, l)};
         ProfScope prof__("norm_times_kernel", st);
-        hipLaunchKernelGGL(norm_times_kernel, norm_grid(ctx, l, 2 * groups), dim3(NT), 0, st, ctx->d_fprimes, v.u(), scaled.u(), l, k, log_n);
+        hipLaunchKernelGGL(norm_times_kernel, norm_grid(ctx, l, 2 * groups), dim3(NT), 0, st, ctx->d_fprimes, v.u(), scaled.u(), l, r.kw, -r.ky, log_n);
         HIP_TRY(ctx, hipGetLastError());
     }
     TRY(rescale_fp(ctx, scaled.u(), 4 * groups, l, wy.u()));
@@ -816,9 +806,8 @@ static int norm_apply(hisa_ctx* ctx, const hisa_tensor* in, const hisa_norm_plan
     const int lw = l;
     const u64* w = wy.u();
     if (!t_analysis) {
-        const StartArgs c = {limb_factors(ctx, r.cw, l), limb_factors(ctx, r.cy, l)};
         ProfScope prof__("norm_start_kernel", st);
-        hipLaunchKernelGGL(norm_start_kernel, norm_grid(ctx, l, 2 * groups), dim3(NT), 0, st, ctx->d_fprimes, wy.u(), l, c, log_n);
+        hipLaunchKernelGGL(norm_start_kernel, norm_grid(ctx, l, 2 * groups), dim3(NT), 0, st, ctx->d_fprimes, wy.u(), l, r.cw, r.cy, log_n);
         HIP_TRY(ctx, hipGetLastError());
     }
     Temp pair(ctx, 2 * groups * words(2, l) * 8), y1(ctx, groups * words(2, l) * 8), y2(ctx, groups * words(2, l) * 8);
@@ -834,8 +823,8 @@ static int norm_apply(hisa_ctx* ctx, const hisa_tensor* in, const hisa_norm_plan
         l -= 1;
         ProductArgs h = product_base(ctx, l);
         h.n_first = (unsigned)groups; h.scaled = 1;
-        h.factor = limb_factors(ctx, step.y, l);
-        h.factor_ab = limb_factors(ctx, -step.product, l);
+        h.factor = step.y;
+        h.factor_ab = -step.product;
         operand_a(h.s[0], {pair.u(), words(2, l), l}, n, 1);
         operand_b(h.s[0], {pair.u() + groups * words(2, l), words(2, l), l}, n);
         operand_add(h.s[0], cy, n);
@@ -850,7 +839,7 @@ static int norm_apply(hisa_ctx* ctx, const hisa_tensor* in, const hisa_norm_plan
     if (t_analysis) TALLY(mul_plain, HISA_OP_MUL_PLAIN, cts, l + 1);
     if (!t_analysis) {
         CentreArgs g = {ctx->d_fprimes, x.base, total.base, (const u64*)p->gamma->ptr, x.bs, (u64)x.limbs * n, total.bs, (u64)total.limbs * n, per,
-                        (unsigned)images, l + 1, centred.u(), limb_factors(ctx, r.count, l + 1)};
+                        (unsigned)images, l + 1, centred.u(), r.count};
         ProfScope prof__("norm_centre_kernel", st);
         hipLaunchKernelGGL(norm_centre_kernel, norm_grid(ctx, l + 1, cts), dim3(NT), 0, st, g, log_n);
         HIP_TRY(ctx, hipGetLastError());
@@ -880,7 +869,7 @@ static int norm_apply(hisa_ctx* ctx, const hisa_tensor* in, const hisa_norm_plan
         operand_a(g.s[0], c, n, 1); operand_b(g.s[0], c, n);
         if (r.act != 0.0) {
             operand_add(g.s[0], c, n);
-            g.factor = limb_factors(ctx, r.act, l);
+            g.factor = r.act;
         }
         TRY(relinearised_products(ctx, g, cts, o.data()));
     }

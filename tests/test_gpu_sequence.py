@@ -366,6 +366,7 @@ def test_refusals():
     refused(DEPTH, n.group_norm_prepare, t, None, None, **dict(good, iterations=3))
     refused(DEPTH, n.group_norm_prepare, t, None, None, **dict(good, act_ratio=0.5, iterations=3))
     refused(SCALE, n.group_norm_prepare, t, None, None, **dict(good, var_lo=1e9, var_hi=1e12))
+    refused(SCALE, n.group_norm_prepare, t, None, None, **dict(good, eps=0.0, var_lo=1e-31, var_hi=1e-30))
     refused(ARG, n.group_norm_prepare, t, np.full(4, 1e12), None, **good)
     refused(ARG, n.group_norm_prepare, t.shaped_like(clean=0), None, None, **good)
     chw = n.tensor_encrypt(np.zeros((1, 4, 3, 3)), 2.0 ** BITS, 8, c_inner=4, c_stride=16)

@@ -155,3 +155,23 @@ def test_geometry_has_the_layout_of_the_header(tmp_path):
                    '    printf("%zu %zu\\n", sizeof(hisa_norm_geom), offsetof(hisa_norm_geom, act));\n    return 0;\n}\n')
     subprocess.check_call(["gcc", "-I", os.path.join(ROOT, "include"), str(src), "-o", str(exe)])
     assert subprocess.check_output([str(exe)]).split() == [b"%d" % ctypes.sizeof(hisa.NormGeom), b"%d" % hisa.NormGeom.act.offset]
+
+
+def test_whole_numbers_as_residues(tmp_path):
+    """fp_whole of csrc/fparith.hpp, compiled for the host, against Python integers: doubles that are whole numbers up to 2^120."""
+    import random
+    src, lib = tmp_path / "w.cpp", tmp_path / "w.so"
+    src.write_text('#include "fparith.hpp"\nextern "C" double whole(double v, double p) { return fp_whole(v, p, 1.0 / p); }\n')
+    inc = os.path.join(ROOT, "paper_1810_00845_amd", "csrc")
+    base = ["g++", "-O2", "-std=c++17", "-ffp-contract=off", "-shared", "-fPIC", "-I", inc, str(src), "-o", str(lib)]
+    if subprocess.run(base[:4] + ["-mfma"] + base[4:], capture_output=True).returncode != 0:
+        subprocess.run(base, check=True)
+    f = ctypes.CDLL(str(lib)).whole
+    f.restype, f.argtypes = ctypes.c_double, [ctypes.c_double] * 2
+    rng = random.Random(1)
+    for p in ((1 << 50) - 27, (1 << 40) - 87, (1 << 30) - 35, 16411):
+        values = [0.0, 1.0, -1.0, 2.0 ** 52, 2.0 ** 53 - 1, -2.0 ** 53, 2.0 ** 53 + 2, 2.0 ** 119, -(2.0 ** 119) * 1.9999]
+        values += [float(int(rng.uniform(-1, 1) * 2.0 ** rng.uniform(0, 120))) for _ in range(2000)]
+        for v in values:
+            r = f(v, float(p))
+            assert r == int(r) and abs(r) <= 0.51 * p and (int(r) - int(v)) % p == 0, (p, v, r)
