@@ -1749,7 +1749,7 @@ __global__ __launch_bounds__(PRODUCT_NT, 4) void product_rows_kernel(ProductArgs
         if (!ROTATED) wide_load<K3>(d, add + s.add_ps, 0, row, t);
     }
     for (uint32_t k = 0; k < terms; k++) {
-        const u64 *a = s.a + (u64)(terms > 1 ? e * terms + k : e / s.a_div) * s.a_bs + limb_at, *b = s.b + (u64)(e * terms + k) * s.b_bs + limb_at;
+        const u64 *a = s.a + (u64)(terms > 1 ? e * terms + k : (e + s.a_skip) / s.a_div) * s.a_bs + limb_at, *b = s.b + (u64)(e * terms + k) * s.b_bs + limb_at;
         if (ROTATED) {
             double a_u[4], b0[4], b1[4];
             wide_load<K3>(a_u, a + u * s.a_ps, 0, row, t);

@@ -269,12 +269,12 @@ u64 galois_of(const hisa_ctx* ctx, int32_t steps);   // 0: a multiple of the slo
 // HISA_ERR_NO_KEY unless both keys of the amount are there (a dry run notes the amount instead)
 int product_keys_present(hisa_ctx* ctx, int32_t steps);
 // Products of ciphertexts and what is added to them, on `limbs` limbs (operands of a higher level need no copy: ps apart are their
-// polynomials, bs their entries):  entry e: factor_ab a b + factor add,  a's entry e / a_div.  Entries from n_first on take
+// polynomials, bs their entries):  entry e: factor_ab a b + factor add,  a's entry (e + a_skip) / a_div.  Entries from n_first on take
 // their operands from s[1].  terms > 1 (entries of s[0], a_div 1): the sum over entries e terms .. of a and of b.
 struct ProductSide {
     const u64 *a, *b, *add;
     u64 a_bs, a_ps, b_bs, b_ps, add_bs, add_ps;
-    unsigned a_div;
+    unsigned a_div, a_skip;
 };
 struct ProductArgs {
     const FpPrime* fprimes;

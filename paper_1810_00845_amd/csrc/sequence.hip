@@ -119,12 +119,23 @@ struct Gathered {      // a tensor's ciphertexts as one strided array for the du
     Gathered(const Gathered&) = delete;
 };
 
-// `entries` products of rotated ciphertexts with their key switches and one division by q_{l-1} P: out [entries][2][l - 1][N].
-// In parts whose extended digits stay below PART_BYTES: more entries at a time would only ask for more memory.
+// Calls go in parts whose extended digits stay below PART_BYTES: more entries at a time would only ask for more memory.  (Parts that fit the
+// last-level cache are slower, their launches being smaller: 38 tokens at N = 2^15, 16 limbs in one part 1.02 ms, in parts of 250 MB 1.40.)
 #define PART_BYTES ((size_t)1 << 30)
-static size_t entries_at_once(const hisa_ctx* ctx, int l) {
-    const size_t digits = ((size_t)l + ctx->alpha - 1) / ctx->alpha, one = 2 * digits * (l + ctx->K) * ctx->N * sizeof(u64);
-    return std::max<size_t>(1, std::min<size_t>(16384, PART_BYTES / one));
+static size_t entries_at_once(const hisa_ctx* ctx, int l, int polys) {
+    const size_t digits = ((size_t)l + ctx->alpha - 1) / ctx->alpha, one = polys * digits * (l + ctx->K) * ctx->N * sizeof(u64);
+    return std::max<size_t>(1, PART_BYTES / one);
+}
+// fn(first, count) over parts of about equal size
+template <class F>
+static int in_parts(size_t entries, size_t most, F fn) {
+    const size_t parts = (entries + most - 1) / most;
+    for (size_t i = 0, e0 = 0; i < parts; i++) {
+        const size_t cnt = (entries - e0 + (parts - i) - 1) / (parts - i);
+        TRY(fn(e0, cnt));
+        e0 += cnt;
+    }
+    return HISA_OK;
 }
 static ProductArgs product_base(const hisa_ctx* ctx, int l) {
     ProductArgs g = {};
@@ -133,40 +144,33 @@ static ProductArgs product_base(const hisa_ctx* ctx, int l) {
     return g;
 }
 // the part [e0, e0 + cnt) of the entries of g
-static ProductArgs product_part(const ProductArgs& g, unsigned e0, unsigned cnt) {
+static ProductArgs product_part(const ProductArgs& g, size_t e0, size_t cnt) {
     ProductArgs r = g;
-    auto skip = [&](ProductSide& s, unsigned by, unsigned terms) {
-        s.a += (u64)(terms > 1 ? by * terms : by / s.a_div) * s.a_bs;
+    auto skip = [&](ProductSide& s, size_t by, size_t terms) {
+        if (terms > 1) s.a += (u64)by * terms * s.a_bs;
+        else s.a_skip += (unsigned)by;
         s.b += (u64)by * terms * s.b_bs;
         if (s.add) s.add += (u64)by * s.add_bs;
     };
     if (e0 < g.n_first) {
         skip(r.s[0], e0, g.terms);
-        r.n_first = std::min(cnt, g.n_first - e0);
+        r.n_first = (unsigned)std::min<size_t>(cnt, g.n_first - e0);
     } else {
         skip(r.s[1], e0 - g.n_first, 1);
         r.n_first = 0;
     }
     return r;
 }
+// products of rotated ciphertexts, or relinearised ones, with their key switches and the rescale: out [entries][2][l - 1][N]
 static int rotated_products(hisa_ctx* ctx, const ProductArgs& g, size_t entries, int32_t step, u64* out) {
-    const size_t n = ctx->N, lw = (size_t)g.limbs * n;
-    TRY(product_keys_present(ctx, step));
-    size_t part = std::min(entries, entries_at_once(ctx, g.limbs));
-    // parts begin where an operand shared by several entries does
-    const size_t unit = std::max(g.s[0].a_div, 1u);
-    if (part < entries && part > unit) part -= part % unit;
-    if (part < entries && (part % unit || g.n_first % unit)) part = 1;
-    for (size_t e0 = 0; e0 < entries; e0 += part) {
-        const unsigned cnt = (unsigned)std::min(part, entries - e0);
-        TRY(rotated_products_fp(ctx, product_part(g, (unsigned)e0, cnt), cnt, step, out + e0 * 2 * (lw - n)));
-    }
-    return HISA_OK;
+    return in_parts(entries, entries_at_once(ctx, g.limbs, 2), [&](size_t e0, size_t cnt) {
+        return rotated_products_fp(ctx, product_part(g, e0, cnt), cnt, step, out + e0 * 2 * (g.limbs - 1) * ctx->N);
+    });
 }
-// products without a rotation, relinearised and rescaled: out [entries][2][l - 1][N]
 static int relinearised_products(hisa_ctx* ctx, const ProductArgs& g, size_t entries, u64* out) {
-    if (entries > 16384) return fail(ctx, HISA_ERR_ARG, "%zu ciphertexts in one call", entries);
-    return products_rescale_fp(ctx, g, entries, out);
+    return in_parts(entries, entries_at_once(ctx, g.limbs, 1), [&](size_t e0, size_t cnt) {
+        return products_rescale_fp(ctx, product_part(g, e0, cnt), cnt, out + e0 * 2 * (g.limbs - 1) * ctx->N);
+    });
 }
 
 // Nothing throws across the C boundary: what the host containers may throw becomes an error code.
@@ -775,11 +779,16 @@ static int norm_apply(hisa_ctx* ctx, const hisa_tensor* in, const hisa_norm_plan
                                squares.u(), log_n);
             HIP_TRY(ctx, hipGetLastError());
         }
-        TRY(relinearize_fp(ctx, squares.u(), groups, l, sum_a.u() + groups * words(2, l)));
+        TRY(in_parts(groups, entries_at_once(ctx, l, 1), [&](size_t e0, size_t cnt) {
+            return relinearize_fp(ctx, squares.u() + e0 * words(3, l), cnt, l, sum_a.u() + (groups + e0) * words(2, l));
+        }));
     }
     u64 *from = sum_a.u(), *to = sum_b.u();
     for (const auto& s : sums) {
-        TRY(rotate_sum_fp(ctx, from, words(2, l), (int)s.size(), s.data(), 2 * groups, l, from, words(2, l), to, true));
+        TRY(in_parts(2 * groups, entries_at_once(ctx, l, 1), [&](size_t e0, size_t cnt) {
+            const u64* part = from + e0 * words(2, l);
+            return rotate_sum_fp(ctx, part, words(2, l), (int)s.size(), s.data(), cnt, l, part, words(2, l), to + e0 * words(2, l), true);
+        }));
         std::swap(from, to);
     }
     const Cts total = {from, words(2, l), l}, total2 = {from + groups * words(2, l), words(2, l), l};

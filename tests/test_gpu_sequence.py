@@ -166,8 +166,7 @@ def test_many_ciphertexts_are_those_of_few():
     from paper_1810_00845_amd import hisa
     g = hisa.Context(12, [50] + [BITS] * 3, 2, 50, 5)
     g.keygen()
-    shared, n = 7, 1204
-    meta = (1, 1, 3, 1, 1)
+    shared, n = 7, 1505
 
     def tensor(cts):
         return hisa.CipherTensor(g, cts, 1, len(cts), 1, 3, 3, 1, 0, 1)
@@ -178,7 +177,28 @@ def test_many_ciphertexts_are_those_of_few():
         few = g.recurrence(tensor(a[i:i + 1]), tensor(x[i * shared:(i + 1) * shared])).cts
         for k in (0, shared - 1):
             assert np.array_equal(g.ct_export(few[k]), g.ct_export(out[i * shared + k]))
-    assert meta
+    for t in (tensor(a), tensor(x)):
+        t.free()
+    # the normalisation's products of 1500 ciphertexts with one 1 / sqrt, in parts that begin inside the group
+    g.close()
+    g = hisa.Context(12, [50] + [BITS] * 7, 2, 50, 5)
+    g.keygen()
+    x = g.ct_random_batch(1500, 8, 2.0 ** BITS, 33)
+    whole = tensor(x)
+    g.gen_rot_keys(g.group_norm_rot_steps(whole))
+    plan = g.group_norm_prepare(whole, None, None, 1, 1e-3, 0.1, 1.0, 1)
+    out = g.group_norm_apply(whole, plan).cts
+    two = g.group_norm_apply(whole.shaped_like(cts=[g.copy(c) for c in x]), plan).cts       # an allocation each
+    for i in (0, 749, 750, 1499):
+        assert np.array_equal(g.ct_export(out[i]), g.ct_export(two[i]))
+    g.group_norm_plan_free(plan)
+    # and against the product that the last part should hold: the same ciphertext twice in a group normalises to the same
+    same_ct = whole.shaped_like(cts=x[:750] + x[:750])
+    plan = g.group_norm_prepare(whole, np.ones(1500), np.zeros(1500), 1, 1e-3, 0.1, 1.0, 1)
+    out = g.group_norm_apply(same_ct, plan).cts
+    for i in (0, 200, 749):
+        assert np.array_equal(g.ct_export(out[i]), g.ct_export(out[750 + i]))
+    g.group_norm_plan_free(plan)
     g.close()
 
 
