@@ -679,9 +679,8 @@ __device__ __forceinline__ void rows_inner(const ConvertArgs& a, const InnerArgs
         if (d < a.n_digits) {
             double v[16];
             if (x >= a.dg[d].own_lo && x < a.dg[d].own_lo + a.dg[d].own_n) {
-                const u64* own = g.own + ct * g.own_bs + (u64)x * n;
-                if constexpr (PAIR) own += d < s.half ? 0 : s.own2;
-                load_row_through<K3>(v, own, galois, row, lane);
+                if constexpr (PAIR) load_row_through<K3>(v, g.own + ct * g.own_bs + (d < s.half ? 0 : s.own2) + (u64)x * n, galois, row, lane);
+                else load_row_through<K3>(v, g.own + ct * g.own_bs + (u64)x * n, galois, row, lane);
                 from_residues(v);
 #pragma unroll
                 for (int r = 0; r < 16; r++) lds[at + ROW_REG(r)] = v[r];
@@ -704,18 +703,16 @@ __device__ __forceinline__ void rows_inner(const ConvertArgs& a, const InnerArgs
             }
         }
         SCHED_FENCE();
+        const double* key_p = (const double*)key + (((u64)d0 * 2 + poly) * a.total + prime) * n + row * 1024u;
         const bool two = d0 + 1 < a.n_digits;
-        const double *key_p, *key_q;
+        rsrc_t k0r = make_rsrc(key_p, 8192u), k1r = make_rsrc(two ? key_p + (u64)2 * a.total * n : key_p, 8192u);
         if constexpr (PAIR) {
             auto key_of = [&](int d) {
                 return (const double*)(d < s.half ? key : s.key2) + (((u64)(d < s.half ? d : d - s.half) * 2 + poly) * a.total + prime) * n + row * 1024u;
             };
-            key_p = key_of(d0); key_q = key_of(d0 + 1);
-        } else {
-            key_p = (const double*)key + (((u64)d0 * 2 + poly) * a.total + prime) * n + row * 1024u;
-            key_q = two ? key_p + (u64)2 * a.total * n : key_p;
+            k0r = make_rsrc(key_of(d0), 8192u);
+            k1r = make_rsrc(key_of(d0 + 1), 8192u);
         }
-        const rsrc_t k0r = make_rsrc(key_p, 8192u), k1r = make_rsrc(key_q, 8192u);
         double k0[16], k1[16];
         load_key_row<ONCE>(k0, k0r, lane);
         // (also without a second digit, then of the first: words left undefined would stay live through the loop)
@@ -931,9 +928,8 @@ __device__ __forceinline__ void wide_rows_inner(const ConvertArgs& a, const Inne
     WideTwiddles w;
     double* slot = lds + part * WIDE_LDS;
     if (own) {
-        const u64* from = g.own + b * g.own_bs + (u64)x * n;
-        if constexpr (PAIR) from += part < s.half ? 0 : s.own2;
-        wide_load<K3>(v, from, g.galois, row, t);
+        if constexpr (PAIR) wide_load<K3>(v, g.own + b * g.own_bs + (part < s.half ? 0 : s.own2) + (u64)x * n, g.galois, row, t);
+        else wide_load<K3>(v, g.own + b * g.own_bs + (u64)x * n, g.galois, row, t);
     } else if (mine) {
         const rsrc_t src = make_rsrc((const double*)a.out + b * a.out_bs + (u64)(a.dg[part].out_pos0 + x) * n + row * 1024u, 8192u);
 #pragma unroll
@@ -945,11 +941,12 @@ __device__ __forceinline__ void wide_rows_inner(const ConvertArgs& a, const Inne
     if (sums) {
 #pragma unroll
         for (int d = 0; d < WIDE_DIGITS; d++) {
-            if (d >= a.n_digits) break;
-            const u64* key = g.key + (((u64)d * 2 + poly) * a.total + prime) * n;
-            if constexpr (PAIR)
-                if (d >= s.half) key = s.key2 + (((u64)(d - s.half) * 2 + poly) * a.total + prime) * n;
-            wide_load<K3>(k[d], key, 0, row, t);
+            if constexpr (PAIR) {
+                const u64* key = d < s.half ? g.key + (((u64)d * 2 + poly) * a.total + prime) * n : s.key2 + (((u64)(d - s.half) * 2 + poly) * a.total + prime) * n;
+                if (d < a.n_digits) wide_load<K3>(k[d], key, 0, row, t);
+            } else {
+                if (d < a.n_digits) wide_load<K3>(k[d], g.key + (((u64)d * 2 + poly) * a.total + prime) * n, 0, row, t);
+            }
         }
         if (with_add) wide_load<K3>(add, g.add + b * g.add_bs + (u64)poly * g.add_ps + (u64)x * n, g.galois, row, t);
         if (MODE == FP_FWD_CONV_SUB) {

@@ -425,20 +425,6 @@ hipError_t launch_key_to_residues(const FpPrime* fprimes, const u64* key, u64* o
     return hipGetLastError();
 }
 
-__global__ __launch_bounds__(NT) void pointwise_mul_kernel(const PrimeConst* primes, const u64* a, const u64* b, u64* out, int log_n) {
-    const PrimeConst pc = primes[blockIdx.y];
-    const u64 at = ((u64)blockIdx.y << log_n) + (u64)blockIdx.x * NT + threadIdx.x;
-    out[at] = mulmod_barrett(a[at], b[at], pc.q, pc.r1, pc.r0);
-}
-
-// out = a b, polynomials over all primes in NTT form
-hipError_t launch_pointwise_mul(const PrimeConst* primes, const u64* a, const u64* b, u64* out, int total, int log_n, hipStream_t st) {
-    DRY_RUN_RETURN();
-    ProfScope prof__("pointwise_mul_kernel", st);
-    hipLaunchKernelGGL(pointwise_mul_kernel, dim3((1u << log_n) / NT, total), dim3(NT), 0, st, primes, a, b, out, log_n);
-    return hipGetLastError();
-}
-
 __global__ __launch_bounds__(NT) void square_kernel(const PrimeConst* primes, const u64* s, u64* out, int log_n) {
     const u64 n = (u64)1 << log_n;
     const PrimeConst pc = primes[blockIdx.y];
@@ -558,5 +544,19 @@ hipError_t launch_reduce_i64(const PrimeConst* primes, const i64* coeffs, u64* o
     dim3 grid((1u << log_n) / NT, limbs, n_pts);
     ProfScope prof__("reduce_i64_kernel", st);
     hipLaunchKernelGGL(reduce_i64_kernel, grid, dim3(NT), 0, st, primes, coeffs, out, out_limbs, log_n);
+    return hipGetLastError();
+}
+
+__global__ __launch_bounds__(NT) void pointwise_mul_kernel(const PrimeConst* primes, const u64* a, const u64* b, u64* out, int log_n) {
+    const PrimeConst pc = primes[blockIdx.y];
+    const u64 at = ((u64)blockIdx.y << log_n) + (u64)blockIdx.x * NT + threadIdx.x;
+    out[at] = mulmod_barrett(a[at], b[at], pc.q, pc.r1, pc.r0);
+}
+
+// out = a b, polynomials over all primes in NTT form
+hipError_t launch_pointwise_mul(const PrimeConst* primes, const u64* a, const u64* b, u64* out, int total, int log_n, hipStream_t st) {
+    DRY_RUN_RETURN();
+    ProfScope prof__("pointwise_mul_kernel", st);
+    hipLaunchKernelGGL(pointwise_mul_kernel, dim3((1u << log_n) / NT, total), dim3(NT), 0, st, primes, a, b, out, log_n);
     return hipGetLastError();
 }

@@ -587,6 +587,7 @@ __device__ __forceinline__ void key_load2(rsrc_t r, uint32_t lane_off, uint32_t 
 // 346), of twelve 531, 721, 1130 / 524, 645, 910; at N = 2^14, 12 limbs eight 116, 151, 229 / 113, 134, 188; of two 139, 180, 268 / 136, 185,
 // 268 and of one 134 / 150 (seven): those stay above.
 #define HALVES_NT 256
+static hipError_t launch_sum_halves(const SumArgs& g, int digits, bool once, hipStream_t st);
 template <int DIGITS, bool ONCE>
 __global__ __launch_bounds__(HALVES_NT, 2) void inner_product_sum_halves_kernel(SumArgs g) {
     const u64 n = (u64)1 << g.log_n;
@@ -744,16 +745,7 @@ hipError_t launch_inner_product_sum_fp(const FpPrime* fprimes, const double* ext
     if (shared_input && n_batch > 2 && !few && digits < 4 && IPS_BCH * ext_bs * 8 <= 0x7fffffffu && ((u64)2 * digits * total << (log_n + 3)) <= 0x7fffffffu) {
         SumArgs g = {fprimes, ext, ext_bs, l, K, L, alpha, n_steps, total, log_n, (uint32_t)n_batch, groups_of_outputs, own_src, c0_src, plain, pmod,
                      own_bs, plain_bs, acc_bs, acc, steps};
-        const dim3 units(8 * ((2 * (l + K) + 7) / 8) * groups_of_outputs * (unsigned)(n / 4 / HALVES_NT));
-        ProfScope prof__("inner_product_sum_halves_kernel", st);
-#define HALVES_LAUNCH(D)                                                                                                 \
-    if (once) hipLaunchKernelGGL((inner_product_sum_halves_kernel<D, true>), units, dim3(HALVES_NT), 0, st, g);          \
-    else hipLaunchKernelGGL((inner_product_sum_halves_kernel<D, false>), units, dim3(HALVES_NT), 0, st, g);                 \
-    return hipGetLastError()
-        if (digits == 1) { HALVES_LAUNCH(1); }
-        if (digits == 2) { HALVES_LAUNCH(2); }
-        HALVES_LAUNCH(3);
-#undef HALVES_LAUNCH
+        return launch_sum_halves(g, digits, once, st);
     }
     ProfScope prof__(once ? "inner_product_sum_once_kernel" : "inner_product_sum_fp_kernel", st);
 #define SUM_LAUNCH(G, D)                                                                                                \
@@ -790,4 +782,18 @@ hipError_t launch_inner_product_steps_fp(const FpPrime* fprimes, const double* e
     hipLaunchKernelGGL(inner_product_steps_fp_kernel, grid, dim3(IPF_NT), 0, st, fprimes, ext, ext_bs, digits, l, K, L, alpha,
                        steps, total, own_src, own_bs, acc, acc_bs, n_batch, c0_src, pmod, log_n);
     return hipGetLastError();
+}
+
+// The last launches of this file, so that their kernels lie behind all others (convert_fp.hip tells why).
+static hipError_t launch_sum_halves(const SumArgs& g, int digits, bool once, hipStream_t st) {
+    const dim3 units(8 * ((2 * (g.l + g.K) + 7) / 8) * g.groups * (1u << (g.log_n - 2)) / HALVES_NT);
+    ProfScope prof__("inner_product_sum_halves_kernel", st);
+#define HALVES_LAUNCH(D)                                                                                                 \
+    if (once) hipLaunchKernelGGL((inner_product_sum_halves_kernel<D, true>), units, dim3(HALVES_NT), 0, st, g);          \
+    else hipLaunchKernelGGL((inner_product_sum_halves_kernel<D, false>), units, dim3(HALVES_NT), 0, st, g);              \
+    return hipGetLastError()
+    if (digits == 1) { HALVES_LAUNCH(1); }
+    if (digits == 2) { HALVES_LAUNCH(2); }
+    HALVES_LAUNCH(3);
+#undef HALVES_LAUNCH
 }
