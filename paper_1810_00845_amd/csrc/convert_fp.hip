@@ -1854,3 +1854,107 @@ hipError_t launch_product_rows_fp(const ProductArgs& g, int log_n, hipStream_t s
 #undef PRODUCT_CASE
     return hipGetLastError();
 }
+
+// ---- the final rows of a division by P whose result is decomposed next (chains of rotations) ----
+// out = (acc - transform) * P^-1 as FP_FWD_CONV_FINAL leaves it; where entry b is a second polynomial (b odd), the row goes on with the
+// inverse rows of the next key switch: mid [entries / 2][ext_limbs][N].  Saves that launch and its reading of what this one wrote.
+template <int K3>
+__device__ __forceinline__ void wide_rows_final_inverse(const ConvertArgs& a, double* mid, int task, double* lds) {
+    const uint32_t t = threadIdx.x, unit = (uint32_t)task / a.n_entries, b = (uint32_t)task - unit * a.n_entries;
+    const uint32_t row = unit & ((1u << K3) - 1);
+    const int e = (int)(unit >> K3);
+    const Modulus q = modulus(a.fprimes, e);
+    constexpr u64 n = (u64)1 << (10 + K3);
+    const rsrc_t dst = make_rsrc(a.out + (u64)b * a.out_bs + (u64)e * n + row * 1024u, 8192u);
+    double v[4], acc[4];
+    WideTwiddles w;
+#pragma unroll
+    for (int r = 0; r < 4; r++) v[r] = bloadf(dst, t * 8u, (uint32_t)r * 2048u);
+    wide_twiddles(w, a.sfwd, a.table_stride, e, row, t, q);
+    wide_load<K3>(acc, a.acc + (u64)b * a.acc_bs + (u64)e * n, 0, row, t);
+    const double pin = as_const(a.pinv_tab)[e];
+    wide_forward(v, COLUMNS_BOUND, w, lds, t, q, 5.2f);
+    if (b & 1) wide_twiddles(w, a.sinv, a.table_stride, e, row, t, q);
+    wide_from_residues(acc);
+#pragma unroll
+    for (int r = 0; r < 4; r++) {
+        v[r] = fp_norm(fp_mulmod(acc[r] - v[r], pin, q.p, q.pinv), q.p, q.pinv);
+        v[r] = v[r] < 0.0 ? v[r] + q.p : v[r];
+        acc[r] = __longlong_as_double((long long)fp_to_u64(v[r]));
+    }
+    wide_store(dst, t, acc);
+    if (!(b & 1)) return;
+    // (from the forward's second stage on the waves keep to their quarters of the row, and so do the inverse's but for the last exchange)
+    wide_inverse(v, 1.0f, w, lds, t, q);
+    const rsrc_t next = make_rsrc(mid + ((u64)(b >> 1) * a.ext_limbs + e) * n + row * 1024u, 8192u);
+#pragma unroll
+    for (int r = 0; r < 4; r++) bstoref(next, t * 8u, (uint32_t)r * 2048u, v[r]);
+}
+template <int K3>
+__global__ __launch_bounds__(WIDE_NT, 4) void final_inverse_wide_kernel(ConvertArgs a, double* mid, int n_tasks) {
+    __shared__ double lds[WIDE_LDS];
+    const int task = wide_task(n_tasks);
+    if (task >= 0) wide_rows_final_inverse<K3>(a, mid, task, lds);
+}
+template <int K3>
+__global__ __launch_bounds__(ROWS_NT, 4) void final_inverse_rows_kernel(ConvertArgs a, double* mid, int n_tasks) {
+    __shared__ double lds_all[ROWS_NT / 64 * ROW_LDS];
+    const int task = row_task(n_tasks);
+    if (task < 0) return;
+    const int lane = threadIdx.x & 63;
+    double* lds = lds_all + (threadIdx.x >> 6) * ROW_LDS;
+    const uint32_t unit = (uint32_t)task / a.n_entries, b = (uint32_t)task - unit * a.n_entries;
+    const uint32_t row = unit & ((1u << K3) - 1);
+    const int e = (int)(unit >> K3);
+    const Modulus q = modulus(a.fprimes, e);
+    constexpr u64 n = (u64)1 << (10 + K3);
+    const rsrc_t dst = make_rsrc(a.out + (u64)b * a.out_bs + (u64)e * n + row * 1024u, 8192u);
+    double v[16], va[16];
+    float m[16];
+    load_row(v, dst, lane);
+#pragma unroll
+    for (int r = 0; r < 16; r++) m[r] = COLUMNS_BOUND;
+    {
+        RowTwiddles w;
+        load_row_twiddles(w, a.sfwd, a.table_stride, e, row, lane);
+        row_forward(v, m, w, lds, lane, q, 5.2f);
+    }
+    load_row(va, make_rsrc(a.acc + (u64)b * a.acc_bs + (u64)e * n + row * 1024u, 8192u), lane);
+    const double pin = as_const(a.pinv_tab)[e];
+    from_residues(va);
+#pragma unroll
+    for (int r = 0; r < 16; r++) {
+        v[r] = fp_norm(fp_mulmod(va[r] - v[r], pin, q.p, q.pinv), q.p, q.pinv);
+        v[r] = v[r] < 0.0 ? v[r] + q.p : v[r];
+        va[r] = __longlong_as_double((long long)fp_to_u64(v[r]));
+        m[r] = 1.0f;
+    }
+    store_row(dst, lane, va);
+    if (!(b & 1)) return;
+    RowTwiddles w;
+    load_row_twiddles(w, a.sinv, a.table_stride, e, row, lane);
+    row_inverse(v, m, w, lds, lane, q);
+    store_row(make_rsrc(mid + ((u64)(b >> 1) * a.ext_limbs + e) * n + row * 1024u, 8192u), lane, v);
+}
+
+hipError_t launch_final_inverse_rows_fp(const ConvertArgs& a, double* mid, hipStream_t st) {
+    DRY_RUN_RETURN();
+    u64 targets = 0;
+    if (a.n_entries == 0 || (a.n_entries & 1) || !convert_args_ok(a, &targets) || !a.acc || !a.pinv_tab || a.add || !mid) return hipErrorInvalidValue;
+    if (a.n_digits != 1 || a.dg[0].own_n || a.dg[0].out_pos0 || a.ext_limbs > a.l) return hipErrorInvalidValue;
+    const u64 tasks = ((u64)a.ext_limbs * a.n_entries) << (a.log_n - 10);
+    const bool wide = tasks <= WIDE_ROWS;
+    const dim3 grid((unsigned)(((wide ? tasks : (tasks + 3) / 4) + 7) / 8 * 8));
+    ProfScope prof__(wide ? "final_inverse_wide_kernel" : "final_inverse_rows_kernel", st);
+#define FINAL_CASE(K3)                                                                                                              \
+    case 10 + K3:                                                                                                                   \
+        if (wide) hipLaunchKernelGGL(final_inverse_wide_kernel<K3>, grid, dim3(WIDE_NT), 0, st, a, mid, (int)tasks);                \
+        else hipLaunchKernelGGL(final_inverse_rows_kernel<K3>, grid, dim3(ROWS_NT), 0, st, a, mid, (int)tasks);                     \
+        break;
+    switch (a.log_n) {
+        FINAL_CASE(2) FINAL_CASE(3) FINAL_CASE(4) FINAL_CASE(5)
+        default: return hipErrorInvalidValue;
+    }
+#undef FINAL_CASE
+    return hipGetLastError();
+}

@@ -1704,6 +1704,56 @@ int rotate_sum_fp(hisa_ctx* ctx, const u64* rot, u64 ct_bs, int n_steps, const i
     return moddown_add_fp(ctx, acc.u(), Bn, l, nullptr, 0, 0, out);
 }
 
+int rotate_sum_chain_fp(hisa_ctx* ctx, u64* from, u64* to, size_t Bn, int l, const std::vector<std::vector<int32_t>>& sums, u64** result) {
+    const size_t n = ctx->N, lw = (size_t)l * n;
+    if (t_analysis || sums.size() < 2) {      // nothing follows anything
+        for (const auto& steps : sums) {
+            TRY(rotate_sum_fp(ctx, from, 2 * lw, (int)steps.size(), steps.data(), Bn, l, from, 2 * lw, to, true));
+            std::swap(from, to);
+        }
+        *result = from;
+        return HISA_OK;
+    }
+    if (!fused_key_switch_available(ctx)) return fail(ctx, HISA_ERR_ARG, "no fused key-switch path for these parameters");
+    const int K = (int)ctx->K, ext_limbs = l + K;
+    FpExt x(ctx, Bn, l, K, (int)ctx->alpha);
+    Temp acc(ctx, Bn * 2 * (size_t)ext_limbs * n * sizeof(u64)), down(ctx, Bn * 2 * (size_t)K * n * sizeof(double));
+    if (!x.ok() || !acc.ok() || !down.ok()) return HISA_ERR_OOM;
+    double *post_q, *post_p;
+    TRY(fp_post_tables(ctx, l, &post_q, &post_p, false));
+    ConvertArgs c = convert_base(ctx, l, Bn);
+    TRY(modup_digits(ctx, c, x, false));
+    c.in = from + lw; c.in_bs = 2 * lw; c.post = post_q;
+    HIP_TRY(ctx, launch_inverse_rows_fp(c, ctx->stream));
+    for (size_t i = 0; i < sums.size(); i++) {
+        IpSteps st = {};
+        const int n_steps = (int)sums[i].size();
+        if (n_steps < 1 || n_steps > FP_MAX_STEPS) return fail(ctx, HISA_ERR_ARG, "bad rotation sum");
+        u64 gs[FP_MAX_STEPS];
+        TRY(rotation_elements(ctx, sums[i].data(), n_steps, gs));
+        for (int s = 0; s < n_steps; s++) { st.key[s] = ctx->keys.find(gs[s])->second.data; st.galois[s] = (uint32_t)gs[s]; }
+        HIP_TRY(ctx, launch_columns_fp(FP_FWD_CONV, c, ctx->stream));
+        HIP_TRY(ctx, launch_forward_rows_fp(FP_FWD_CONV, c, ctx->stream));
+        HIP_TRY(ctx, launch_inner_product_sum_fp(ctx->tabs.fprimes, x.extp, x.ext_bs, x.digits, l, K, (int)ctx->L, (int)ctx->alpha, st, n_steps, (int)ctx->total,
+                                                 from + lw, 2 * lw, acc.u(), (u64)2 * ext_limbs * n, Bn, 1, from, from, 2 * lw, ctx->d_pmod, (int)ctx->log_n,
+                                                 ctx->stream));
+        ConvertArgs m = convert_base(ctx, l, Bn * 2);      // entries are (ciphertext, b|a) pairs
+        m.in = acc.u(); m.in_bs = (u64)ext_limbs * n; m.src_pos0 = l; m.n_src = K; m.post = post_p; m.mid = down.as<double>();
+        m.n_digits = 1; m.dg[0] = {ctx->moddown_tab->d_hat_f, 0, K, 0, 0, 0}; m.ext_limbs = l; m.out = to; m.out_bs = lw;
+        m.acc = acc.u(); m.acc_bs = (u64)ext_limbs * n; m.pinv_tab = ctx->d_pinv_f;
+        if (i + 1 == sums.size()) {
+            TRY(divide_fp(ctx, m));
+        } else {
+            HIP_TRY(ctx, launch_inverse_rows_fp(m, ctx->stream));
+            HIP_TRY(ctx, launch_columns_fp(FP_FWD_CONV_FINAL, m, ctx->stream));
+            HIP_TRY(ctx, launch_final_inverse_rows_fp(m, x.yp, ctx->stream));
+        }
+        std::swap(from, to);
+    }
+    *result = from;
+    return HISA_OK;
+}
+
 extern "C" int hisa_set_fused_rescale(hisa_ctx* ctx, uint32_t on) {
     if (!ctx) return HISA_ERR_ARG;
     if (on > 1) return fail(ctx, HISA_ERR_ARG, "on is 0 or 1");

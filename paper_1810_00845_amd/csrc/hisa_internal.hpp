@@ -223,6 +223,9 @@ int rotation_accumulators_fp(hisa_ctx* ctx, const u64* cts, u64 ct_bs, size_t B,
 // rescale: the sum's divScalar is taken together with its division by P (moddown_rescale_fp): out [Bn][2][l - 1][N].
 int rotate_sum_fp(hisa_ctx* ctx, const u64* rot, u64 ct_bs, int n_steps, const int32_t* steps, size_t Bn, int l,
                   const u64* plain, u64 plain_bs, u64* out, bool shared_input = false, bool rescale = false);
+// A chain of them: x <- x + sum_s rotLeft(x, steps[s]) for one list of amounts after the other, Bn ciphertexts [2][l][N] side by side in
+// `from`; `from` and `to` take turns and *result is the one that holds the last sums.
+int rotate_sum_chain_fp(hisa_ctx* ctx, u64* from, u64* to, size_t Bn, int l, const std::vector<std::vector<int32_t>>& sums, u64** result);
 // What a kernel that forms the accumulators of rotations itself reads: the extended digits of B ciphertexts, transformed (ext), the
 // keys and automorphisms of the rotations (st)
 struct IpSteps;
@@ -428,6 +431,9 @@ struct ConvertArgs {
 hipError_t launch_inverse_rows_fp(const ConvertArgs& a, hipStream_t st);              // in -> mid
 hipError_t launch_columns_fp(int mode, const ConvertArgs& a, hipStream_t st);         // mid -> out (modes 3, 4, 6)
 hipError_t launch_forward_rows_fp(int mode, const ConvertArgs& a, hipStream_t st);    // out, in place (modes 3, 4, 7)
+// FP_FWD_CONV_FINAL's rows (one digit, no addend, entries in (b, a) pairs) that go on with the inverse rows of the a polynomials: mid
+// [n_entries / 2][ext_limbs][N] is what the columns of their next key switch read
+hipError_t launch_final_inverse_rows_fp(const ConvertArgs& a, double* mid, hipStream_t st);
 // The rows behind the columns of a key switch's digits (ConvertArgs::out: [n_entries][digits][ext_limbs][N]), with the inner
 // product with `key` and the neighbouring halves of the division that follows, for the limbs x_begin .. x_end - 1.
 // FP_INV_D_TO_Y: limbs from n_acc on are sources of that division: down [n_entries * 2][ext_limbs - n_acc][N] =

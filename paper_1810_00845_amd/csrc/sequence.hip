@@ -783,14 +783,13 @@ static int norm_apply(hisa_ctx* ctx, const hisa_tensor* in, const hisa_norm_plan
             return relinearize_fp(ctx, squares.u() + e0 * words(3, l), cnt, l, sum_a.u() + (groups + e0) * words(2, l));
         }));
     }
-    u64 *from = sum_a.u(), *to = sum_b.u();
-    for (const auto& s : sums) {
-        TRY(in_parts(2 * groups, entries_at_once(ctx, l, 1), [&](size_t e0, size_t cnt) {
-            const u64* part = from + e0 * words(2, l);
-            return rotate_sum_fp(ctx, part, words(2, l), (int)s.size(), s.data(), cnt, l, part, words(2, l), to + e0 * words(2, l), true);
-        }));
-        std::swap(from, to);
-    }
+    u64* from = nullptr;      // where the last sums are: in the same of the two for every part
+    TRY(in_parts(2 * groups, entries_at_once(ctx, l, 1), [&](size_t e0, size_t cnt) {
+        u64* part = nullptr;
+        TRY(rotate_sum_chain_fp(ctx, sum_a.u() + e0 * words(2, l), sum_b.u() + e0 * words(2, l), cnt, l, sums, &part));
+        if (e0 == 0) from = part;
+        return HISA_OK;
+    }));
     const Cts total = {from, words(2, l), l}, total2 = {from + groups * words(2, l), words(2, l), l};
     // V = n sum x^2 - (sum x)^2
     Temp v(ctx, groups * words(2, l - 1) * 8), scaled(ctx, 2 * groups * words(2, l - 1) * 8), wy(ctx, 2 * groups * words(2, l - 2) * 8);
