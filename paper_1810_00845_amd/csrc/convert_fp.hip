@@ -679,7 +679,7 @@ __device__ __forceinline__ void rows_inner(const ConvertArgs& a, const InnerArgs
         if (d < a.n_digits) {
             double v[16];
             if (x >= a.dg[d].own_lo && x < a.dg[d].own_lo + a.dg[d].own_n) {
-                if constexpr (PAIR) load_row_through<K3>(v, g.own + ct * g.own_bs + (d < s.half ? 0 : s.own2) + (u64)x * n, galois, row, lane);
+                if constexpr (PAIR) load_row_through<K3>(v, g.own + ct * g.own_bs + (d & 1 ? s.own2 : 0) + (u64)x * n, galois, row, lane);
                 else load_row_through<K3>(v, g.own + ct * g.own_bs + (u64)x * n, galois, row, lane);
                 from_residues(v);
 #pragma unroll
@@ -708,7 +708,7 @@ __device__ __forceinline__ void rows_inner(const ConvertArgs& a, const InnerArgs
         rsrc_t k0r = make_rsrc(key_p, 8192u), k1r = make_rsrc(two ? key_p + (u64)2 * a.total * n : key_p, 8192u);
         if constexpr (PAIR) {
             auto key_of = [&](int d) {
-                return (const double*)(d < s.half ? key : s.key2) + (((u64)(d < s.half ? d : d - s.half) * 2 + poly) * a.total + prime) * n + row * 1024u;
+                return (const double*)(d & 1 ? s.key2 : key) + (((u64)(d & ~1) + poly) * a.total + prime) * n + row * 1024u;
             };
             k0r = make_rsrc(key_of(d0), 8192u);
             k1r = make_rsrc(key_of(d0 + 1), 8192u);
@@ -928,7 +928,7 @@ __device__ __forceinline__ void wide_rows_inner(const ConvertArgs& a, const Inne
     WideTwiddles w;
     double* slot = lds + part * WIDE_LDS;
     if (own) {
-        if constexpr (PAIR) wide_load<K3>(v, g.own + b * g.own_bs + (part < s.half ? 0 : s.own2) + (u64)x * n, g.galois, row, t);
+        if constexpr (PAIR) wide_load<K3>(v, g.own + b * g.own_bs + (part & 1 ? s.own2 : 0) + (u64)x * n, g.galois, row, t);
         else wide_load<K3>(v, g.own + b * g.own_bs + (u64)x * n, g.galois, row, t);
     } else if (mine) {
         const rsrc_t src = make_rsrc((const double*)a.out + b * a.out_bs + (u64)(a.dg[part].out_pos0 + x) * n + row * 1024u, 8192u);
@@ -942,7 +942,7 @@ __device__ __forceinline__ void wide_rows_inner(const ConvertArgs& a, const Inne
 #pragma unroll
         for (int d = 0; d < WIDE_DIGITS; d++) {
             if constexpr (PAIR) {
-                const u64* key = d < s.half ? g.key + (((u64)d * 2 + poly) * a.total + prime) * n : s.key2 + (((u64)(d - s.half) * 2 + poly) * a.total + prime) * n;
+                const u64* key = (d & 1 ? s.key2 : g.key) + (((u64)(d & ~1) + poly) * a.total + prime) * n;
                 if (d < a.n_digits) wide_load<K3>(k[d], key, 0, row, t);
             } else {
                 if (d < a.n_digits) wide_load<K3>(k[d], g.key + (((u64)d * 2 + poly) * a.total + prime) * n, 0, row, t);
@@ -1657,9 +1657,9 @@ static hipError_t launch_step_rows_once(int mode, dim3 grid, const ConvertArgs& 
 }
 
 // ---- pairs: two polynomials with a key each, one accumulator, one division (products of rotated ciphertexts) ----
-// The digits of the second polynomial stand behind those of the first (a.n_digits counts both, at most FP_MAX_DIGITS); the same rows as
-// above otherwise.  Two waves a task have both something to transform in every round where one polynomial of three digits leaves
-// one of them idle in the second.
+// Digit d of the 2 half that a.n_digits counts (at most FP_MAX_DIGITS) is digit d / 2 of the first polynomial or, d odd, of the second:
+// of the two waves of a task each has a polynomial's digits, and the round of a limb's own digits, which need no transform, is the same
+// for both.  The first polynomial's digits in front of the second's have one wave wait for the other in two rounds of three.
 template <int K3, int MODE>
 __global__ __launch_bounds__(128, 4) void inner_product_pair_rows_kernel(ConvertArgs a, InnerArgs g, PairArgs s, int n_tasks) {
     __shared__ double lds[2 * ROW_LDS];
@@ -1693,7 +1693,7 @@ hipError_t launch_inner_pair_rows_fp(int mode, const ConvertArgs& a, const Inner
     DRY_RUN_RETURN();
     u64 targets = 0;
     const u64 n = (u64)1 << a.log_n;
-    if (a.n_entries == 0 || !convert_args_ok(a, &targets) || s.half < 1 || a.n_digits != 2 * s.half) return hipErrorInvalidValue;
+    if (a.n_entries == 0 || !convert_args_ok(a, &targets) || (a.n_digits & 1)) return hipErrorInvalidValue;
     if (!g.key || !s.key2 || !g.own || !g.c1 || g.galois || g.n_acc < 1 || g.n_acc >= a.ext_limbs || g.n_acc > a.l) return hipErrorInvalidValue;
     if (g.x_begin < 0 || g.x_begin >= g.x_end || g.x_end > a.ext_limbs || g.own_bs < s.own2 + (u64)a.l * n || s.own2 < (u64)a.l * n)
         return hipErrorInvalidValue;

@@ -2019,15 +2019,15 @@ int rotated_products_fp(hisa_ctx* ctx, const ProductArgs& g_in, size_t n_pairs, 
     Temp acc(ctx, poly * (size_t)by.n_acc, stored), down(ctx, poly * (size_t)(ext_limbs - by.n_acc));
     if ((stored && !acc.ok()) || !down.ok()) return HISA_ERR_OOM;
     c.n_entries = (unsigned)n_pairs; c.n_digits = 2 * x.digits; c.out_bs = 2 * x.ext_bs;
-    for (int d = 0; d < x.digits; d++) {
-        c.dg[x.digits + d] = c.dg[d];
-        c.dg[x.digits + d].out_pos0 += x.digits * ext_limbs;
+    for (int d = x.digits - 1; d >= 0; d--) {      // the digits of the two take turns
+        c.dg[2 * d] = c.dg[2 * d + 1] = c.dg[d];
+        c.dg[2 * d + 1].out_pos0 += x.digits * ext_limbs;
     }
     InnerArgs r = {};
     r.key = key.data; r.own = pairs.u(); r.own_bs = 2 * lw;
     r.add = plain.u(); r.add_bs = 2 * lw; r.add_ps = lw; r.add_polys = 2;
     r.acc = stored ? acc.as<double>() : nullptr; r.down = down.as<double>();
-    const PairArgs second = {key2.data, lw, x.digits};
+    const PairArgs second = {key2.data, lw};
     return key_switch_divide_fp(ctx, c, r, by, nullptr, &second, l, n_pairs, out);
 }
 

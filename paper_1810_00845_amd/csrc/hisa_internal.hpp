@@ -465,12 +465,11 @@ struct StepArgs {
     unsigned step_B;
     IpSteps steps;
 };
-// The same for pairs of polynomials with a key each and one accumulator: a.n_digits = 2 half, the digits of the second behind those of the
-// first in an entry of a.out, its own digits own2 words behind the first's, its key key2.
+// The same for pairs of polynomials with a key each and one accumulator: the digits of the two take turns in a.dg (a.n_digits counts both), the
+// second's own digits lie own2 words behind the first's, its key is key2.
 struct PairArgs {
     const u64* key2;
     u64 own2;
-    int half;
 };
 hipError_t launch_inner_pair_rows_fp(int mode, const ConvertArgs& a, const InnerArgs& g, const PairArgs& s, hipStream_t st);
 hipError_t launch_inner_rows_fp(int mode, const ConvertArgs& a, const InnerArgs& g, const StepArgs* steps, hipStream_t st);
