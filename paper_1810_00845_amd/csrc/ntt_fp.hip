@@ -582,7 +582,7 @@ __device__ __forceinline__ void key_load2(rsrc_t r, uint32_t lane_off, uint32_t 
 // uniform branch, and a thread owns two neighbouring coefficients, which an automorphism leaves neighbours.  An XCD keeps to one half of
 // a limb at a time -- an automorphism moves no value across the halves -- with the groups of outputs of a block next to each other.
 // Seven rotations of eight outputs at N = 2^15, 28 limbs 221 -> 191 us (a coefficient a thread 206): 36 to 40 million vector instructions for
-// 56, and 6.4 TB/s of what the L2 passes on (keys 308 MB, digits 172 MB, each group of four outputs its own).  Whole sums, us, as
+// 56, and 9 to 10 million misses of the L2 (keys 308 MB, digits 172 MB), which bound it.  Whole sums, us, as
 // above / here: of four outputs at N = 2^15, 21 limbs, 3, 7 and 15 rotations 225, 286, 422 / 217, 273, 379 (keys past the caches: 207, 256,
 // 346), of twelve 531, 721, 1130 / 524, 645, 910; at N = 2^14, 12 limbs eight 116, 151, 229 / 113, 134, 188; of two 139, 180, 268 / 136, 185,
 // 268 and of one 134 / 150 (seven): those stay above.
