@@ -366,7 +366,8 @@ static int recurrence_grad(hisa_ctx* ctx, const hisa_tensor* gates, const hisa_t
     TRY(check_gates(ctx, gates, grad, &shared));
     TRY(check_gates(ctx, h, grad, &same));
     if (same != 1) return fail(ctx, HISA_ERR_ARG, "states and gradients have different channels");
-    if (!dx || !dx->cts || !dgates || !dgates->cts) return fail(ctx, HISA_ERR_ARG, "bad output tensor");
+    if (!dx || !dx->cts || !dgates || !dgates->cts || dx->cts == dgates->cts)
+        return fail(ctx, HISA_ERR_ARG, "bad output tensor");
     TRY(need_fused(ctx, "a recurrence"));
     TRY(check_clean(ctx, gates, "gates of a recurrence"));
     TRY(check_clean(ctx, grad, "gradients of a recurrence"));

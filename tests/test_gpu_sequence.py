@@ -1,5 +1,7 @@
 """GPU: recurrences and group normalisation through the C ABI, bit for bit against the oracle, decrypted against plain fp64 arrays,
 and what they refuse."""
+import ctypes as C
+
 import numpy as np
 import pytest
 
@@ -315,6 +317,22 @@ def test_a_block_of_both():
     g.close()
 
 
+@pytest.mark.parametrize("limbs,dnum", [(12, 3), (12, 1), (11, 2)])
+def test_rotation_sums_of_a_ragged_number(limbs, dnum):
+    """Sums of rotations of three and more ciphertexts, the last group of outputs part filled, against one at a time."""
+    from paper_1810_00845_amd import hisa
+    g = hisa.Context(15, [50] + [BITS] * (limbs - 1), dnum, 50, 5)
+    steps = [0, 1, 2, 3, 4, 5, 6, 7]
+    g.gen_rot_keys(steps[1:])
+    cts = g.ct_random_batch(7, limbs, 2.0 ** BITS, 3)
+    one = [g.ct_export(g.rot_left_sum_batch([[c]] * 8, steps)[0]) for c in cts]
+    for n in (3, 5, 6, 7):
+        some = [g.copy(c) for c in cts[7 - n:]] if n == 5 else cts[7 - n:]      # an allocation each, views of one
+        for got, want in zip(g.rot_left_sum_batch([some] * 8, steps), one[7 - n:]):
+            assert np.array_equal(g.ct_export(got), want)
+    g.close()
+
+
 # --- dry runs and refusals ---
 
 def test_dry_run_names_keys_and_levels():
@@ -367,6 +385,9 @@ def test_refusals():
     refused(ARG, g.recurrence, a, x.shaped_like(w_stride=0, h_stride=0))
     one = tensor(width=1)
     refused(ARG, g.recurrence_grad, one, one, one)
+    both = x.shaped_like()      # one output for two gradients
+    (st, _arr), (xs, _brr) = both._struct(), x._struct()
+    assert hisa.load().hisa_recurrence_grad(g._vp, C.byref(xs), C.byref(xs), C.byref(xs), C.c_uint32(0), C.byref(st), C.byref(st)) == ARG
     refused(SCALE, g.recurrence, tensor(scale=2.0 ** 9.5), x)
     refused(SCALE, g.recurrence_step, tensor(scale=2.0 ** 3), tensor(scale=2.0 ** 3), x)
     mixed = x.shaped_like(cts=[x.cts[0], tensor(scale=2.0 ** 39).cts[0]])
