@@ -615,6 +615,8 @@ __global__ __launch_bounds__(HALVES_NT, 2) void inner_product_sum_halves_kernel(
     auto fold = [&](FpSum& s) { s = FpSum{plan.base, fp_norm(fp_sum_value(s, plan.base, p, pinv), p, pinv)}; };
     int pending = 0, c0_pending = 0;
     const uint32_t key_bytes = (uint32_t)(2 * DIGITS * g.total) * row;
+    // outputs beyond the last one read that one's values again: a resource's bounds are not asked to cover the scalar offset
+    auto entry = [&](int u) { return (uint32_t)(u < live ? u : live - 1); };
     for (int s = 0; s < g.n_steps; s++) {
         const rsrc_t key_r = make_rsrc((const double*)g.steps.key[s] + (u64)prime * n, key_bytes - (uint32_t)prime * row);
         const uint32_t from = galois_src_fp(j, g.steps.galois[s], g.log_n);
@@ -630,15 +632,15 @@ __global__ __launch_bounds__(HALVES_NT, 2) void inner_product_sum_halves_kernel(
         for (int d = 0; d < DIGITS; d++) {
             if (d == own) {
 #pragma unroll
-                for (int u = 0; u < IPS_BCH; u++) bload2(own_r, src, (uint32_t)u * own_u, e[d][u][0], e[d][u][1]);      // beyond the last output: zero
+                for (int u = 0; u < IPS_BCH; u++) bload2(own_r, src, entry(u) * own_u, e[d][u][0], e[d][u][1]);
             } else {
 #pragma unroll
-                for (int u = 0; u < IPS_BCH; u++) bload2(ext_r, src, (uint32_t)u * ext_u + (uint32_t)(d * ext_limbs) * row, e[d][u][0], e[d][u][1]);
+                for (int u = 0; u < IPS_BCH; u++) bload2(ext_r, src, entry(u) * ext_u + (uint32_t)(d * ext_limbs) * row, e[d][u][0], e[d][u][1]);
             }
         }
         if (x < g.l) {
 #pragma unroll
-            for (int u = 0; u < IPS_BCH; u++) bload2(c0_r, src, (uint32_t)u * own_u, c0[u][0], c0[u][1]);
+            for (int u = 0; u < IPS_BCH; u++) bload2(c0_r, src, entry(u) * own_u, c0[u][0], c0[u][1]);
         }
 #pragma unroll
         for (int d = 0; d < DIGITS; d++) {
@@ -742,7 +744,8 @@ hipError_t launch_inner_product_sum_fp(const FpPrime* fprimes, const double* ext
     dim3 grid((1u << log_n) / (few ? 64 : IPF_NT), groups_of_outputs, l + K);
     const bool once = groups_of_outputs == 1 && ((u64)n_steps * digits * 2 * (l + K) << (log_n + 3)) > STREAMED_KEY_BYTES;
     // rotations of three outputs and more, up to three digits known to the compiler, offsets that fit a buffer resource
-    if (shared_input && n_batch > 2 && !few && digits < 4 && IPS_BCH * ext_bs * 8 <= 0x7fffffffu && ((u64)2 * digits * total << (log_n + 3)) <= 0x7fffffffu) {
+    if (shared_input && n_batch > 2 && !few && digits < 4 && IPS_BCH * (ext_bs > own_bs ? ext_bs : own_bs) * 8 <= 0x7fffffffu &&
+        ((u64)2 * digits * total << (log_n + 3)) <= 0x7fffffffu) {
         SumArgs g = {fprimes, ext, ext_bs, l, K, L, alpha, n_steps, total, log_n, (uint32_t)n_batch, groups_of_outputs, own_src, c0_src, plain, pmod,
                      own_bs, plain_bs, acc_bs, acc, steps};
         return launch_sum_halves(g, digits, once, st);
