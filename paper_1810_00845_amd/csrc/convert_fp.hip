@@ -1741,9 +1741,9 @@ __global__ __launch_bounds__(PRODUCT_NT, 4) void product_rows_kernel(ProductArgs
     double x[4] = {}, y[4] = {}, c[4], d[4];
     WideTwiddles w;
     if (s.add && (ROTATED || !u)) {
-        const u64* add = s.add + (u64)e * s.add_bs + limb_at;
+        const u64* add = s.add + (u64)(!ROTATED && g.plain_period ? (e + s.a_skip) % g.plain_period : e) * s.add_bs + limb_at;
         wide_load<K3>(c, add + (ROTATED ? u : 0) * s.add_ps, 0, row, t);
-        if (!ROTATED) wide_load<K3>(d, add + s.add_ps, 0, row, t);
+        if (!ROTATED && !g.plain_period) wide_load<K3>(d, add + s.add_ps, 0, row, t);
     }
     for (uint32_t k = 0; k < terms; k++) {
         const u64 *a = s.a + (u64)(terms > 1 ? e * terms + k : (e + s.a_skip) / s.a_div) * s.a_bs + limb_at, *b = s.b + (u64)(e * terms + k) * s.b_bs + limb_at;
@@ -1798,7 +1798,7 @@ __global__ __launch_bounds__(PRODUCT_NT, 4) void product_rows_kernel(ProductArgs
         wide_from_residues(c);
 #pragma unroll
         for (int r = 0; r < 4; r++) x[r] += fp_mulmod(c[r], f, q.p, q.pinv);
-        if (!ROTATED) {
+        if (!ROTATED && !g.plain_period) {
             wide_from_residues(d);
 #pragma unroll
             for (int r = 0; r < 4; r++) y[r] += fp_mulmod(d[r], f, q.p, q.pinv);
@@ -1830,14 +1830,14 @@ __global__ __launch_bounds__(PRODUCT_NT, 4) void product_rows_kernel(ProductArgs
 hipError_t launch_product_rows_fp(const ProductArgs& g, int log_n, hipStream_t st) {
     DRY_RUN_RETURN();
     if (!g.fprimes || !g.out || !g.mid || !g.sinv || (g.galois && !g.pairs) || g.limbs < 1 || g.n_entries < 1 || g.n_first > (unsigned)g.n_entries ||
-        g.terms < 1 || (g.galois && g.scaled))
+        g.terms < 1 || (g.galois && (g.scaled || g.plain_period)))
         return hipErrorInvalidValue;
     const u64 n = (u64)1 << log_n, tasks = ((u64)g.limbs * g.n_entries) << (log_n - 10);
     if (log_n < 12 || log_n > 15 || tasks > 0x7fffff00u) return hipErrorInvalidValue;
     for (int i = 0; i < 2; i++) {
         const ProductSide& s = g.s[i];
         if (i == 0 ? g.n_first == 0 : g.n_first == (unsigned)g.n_entries) continue;
-        if (!s.a || !s.b || s.a_div < 1 || s.a_ps < (u64)g.limbs * n || s.b_ps < (u64)g.limbs * n || (s.add && s.add_ps < (u64)g.limbs * n))
+        if (!s.a || !s.b || s.a_div < 1 || s.a_ps < (u64)g.limbs * n || s.b_ps < (u64)g.limbs * n || (s.add && (g.plain_period ? s.add_bs : s.add_ps) < (u64)g.limbs * n))
             return hipErrorInvalidValue;
     }
     const dim3 grid((unsigned)((tasks + 7) / 8 * 8));

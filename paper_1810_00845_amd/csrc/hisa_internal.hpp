@@ -273,7 +273,8 @@ u64 galois_of(const hisa_ctx* ctx, int32_t steps);   // 0: a multiple of the slo
 int product_keys_present(hisa_ctx* ctx, int32_t steps);
 // Products of ciphertexts and what is added to them, on `limbs` limbs (operands of a higher level need no copy: ps apart are their
 // polynomials, bs their entries):  entry e: factor_ab a b + factor add,  a's entry (e + a_skip) / a_div.  Entries from n_first on take
-// their operands from s[1].  terms > 1 (entries of s[0], a_div 1): the sum over entries e terms .. of a and of b.
+// their operands from s[1].  plain_period: add holds plaintexts [plain_period][limbs][N], entry (e + a_skip) % plain_period, for the first
+// polynomial of products without a rotation.  terms > 1 (entries of s[0], a_div 1): the sum over entries e terms .. of a and of b.
 struct ProductSide {
     const u64 *a, *b, *add;
     u64 a_bs, a_ps, b_bs, b_ps, add_bs, add_ps;
@@ -282,7 +283,7 @@ struct ProductSide {
 struct ProductArgs {
     const FpPrime* fprimes;
     ProductSide s[2];
-    unsigned n_first, terms;
+    unsigned n_first, terms, plain_period;
     int limbs, scaled;                   // scaled: by factor_ab (products without a rotation)
     u64 galois;                          // of b; 0: none
     double factor, factor_ab;            // whole numbers below 2^120

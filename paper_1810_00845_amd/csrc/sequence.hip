@@ -150,7 +150,7 @@ static ProductArgs product_part(const ProductArgs& g, size_t e0, size_t cnt) {
         if (terms > 1) s.a += (u64)by * terms * s.a_bs;
         else s.a_skip += (unsigned)by;
         s.b += (u64)by * terms * s.b_bs;
-        if (s.add) s.add += (u64)by * s.add_bs;
+        if (s.add && !g.plain_period) s.add += (u64)by * s.add_bs;
     };
     if (e0 < g.n_first) {
         skip(r.s[0], e0, g.terms);
@@ -485,23 +485,19 @@ __global__ __launch_bounds__(NT) void group_moments_kernel(const FpPrime* fprime
     out3[group * 3 * lw + 2 * lw + at] = fp_canonical(s11, p, pinv);
 }
 
-// k_w x and -k_y x side by side: the variances, polynomials [polys][limbs][N], on their way to two scales
-__global__ __launch_bounds__(NT) void norm_times_kernel(const FpPrime* fprimes, const u64* x, u64* out, int limbs, double kw, double ky, int log_n) {
+// k_w x + c_w q and -k_y x + c_y q side by side: the variances, polynomials [2 groups][limbs][N], on their way to two scales, with constants
+// (at every evaluation point the same, of first polynomials) that the division by q leaves as c_w and c_y
+__global__ __launch_bounds__(NT) void norm_times_kernel(const FpPrime* fprimes, const u64* x, u64* out, int limbs, double kw, double ky, double cw, double cy,
+                                                        double last, int log_n) {
     const int limb = blockIdx.y;
     const u64 at = (((u64)blockIdx.z * limbs + limb) << log_n) + (u64)blockIdx.x * NT + threadIdx.x;
     const double p = as_const(&fprimes[limb].p)[0], pinv = as_const(&fprimes[limb].p)[1], half = as_const(&fprimes[limb].p)[2];
     const double v = fp_centred_from_u64(x[at], p, half);
-    out[at] = fp_canonical(fp_mulmod(v, fp_whole(kw, p, pinv), p, pinv), p, pinv);
-    out[at + (((u64)gridDim.z * limbs) << log_n)] = fp_canonical(fp_mulmod(v, fp_whole(ky, p, pinv), p, pinv), p, pinv);
-}
-
-// The first polynomials of w and of y plus a constant each, in place (a constant polynomial is that constant at every evaluation point):
-// entries [2 groups], w in front
-__global__ __launch_bounds__(NT) void norm_start_kernel(const FpPrime* fprimes, u64* x, int limbs, double cw, double cy, int log_n) {
-    const int limb = blockIdx.y;
-    const u64 at = (((u64)blockIdx.z * 2 * limbs + limb) << log_n) + (u64)blockIdx.x * NT + threadIdx.x;
-    const double p = as_const(&fprimes[limb].p)[0], pinv = as_const(&fprimes[limb].p)[1];
-    x[at] = fp_canonical(fp_from_u64(x[at]) + (2 * blockIdx.z < gridDim.z ? fp_whole(cw, p, pinv) : fp_whole(cy, p, pinv)), p, pinv);
+    const double q = blockIdx.z & 1 ? 0.0 : fp_whole(last, p, pinv);
+    const double w = fp_mulmod(v, fp_whole(kw, p, pinv), p, pinv) + fp_mulmod(q, fp_whole(cw, p, pinv), p, pinv);
+    const double y = fp_mulmod(v, fp_whole(ky, p, pinv), p, pinv) + fp_mulmod(q, fp_whole(cy, p, pinv), p, pinv);
+    out[at] = fp_canonical(w, p, pinv);
+    out[at + (((u64)gridDim.z * limbs) << log_n)] = fp_canonical(y, p, pinv);
 }
 
 // out = (n x - m) gamma: x entry e, m entry e / per, gamma plaintext e % images, on the first `limbs` limbs
@@ -527,15 +523,6 @@ __global__ __launch_bounds__(NT) void norm_centre_kernel(CentreArgs g, int log_n
         const double d = fp_norm(fp_mulmod(x, count, p, pinv) - m, p, pinv);
         g.out[(e * 2 + poly) * lw + at] = fp_canonical(fp_mulmod(d, w, p, pinv), p, pinv);
     }
-}
-
-// first polynomials += plaintext e % period
-__global__ __launch_bounds__(NT) void norm_shift_kernel(const FpPrime* fprimes, u64* x, const u64* beta, unsigned period, int limbs, int log_n) {
-    const u64 n = (u64)1 << log_n, lw = (u64)limbs * n;
-    const int limb = blockIdx.y;
-    const u64 e = blockIdx.z, at = (u64)limb * n + (u64)blockIdx.x * NT + threadIdx.x;
-    const double p = as_const(&fprimes[limb].p)[0], pinv = as_const(&fprimes[limb].p)[1];
-    x[e * 2 * lw + at] = fp_canonical(fp_from_u64(x[e * 2 * lw + at]) + fp_from_u64(beta[(e % period) * lw + at]), p, pinv);
 }
 
 static dim3 norm_grid(const hisa_ctx* ctx, int limbs, size_t entries) { return dim3(ctx->N / NT, limbs, (unsigned)entries); }
@@ -689,7 +676,7 @@ static int norm_prepare(hisa_ctx* ctx, const hisa_tensor* like, const double* ga
     NormSchedule full;
     TRY(norm_schedule(ctx, *geom, n, level, s, gamma_scale, &full));
     const uint32_t ci = t_ci(like), per = (uint32_t)t_per(like);
-    const size_t hw = (size_t)like->height * like->width, lg = (size_t)full.level_y + 1, lb = (size_t)full.level_y - 1;
+    const size_t hw = (size_t)like->height * like->width, lg = (size_t)full.level_y + 1, lb = (size_t)full.level_y;
     hisa_norm_plan* p = new hisa_norm_plan{HISA_MAGIC_NORMPLAN, like->channels, like->height, like->width, like->h_stride, like->w_stride, like->offset,
                                            ci, like->c_stride, (uint32_t)level, s, *geom, gamma_scale, nullptr, nullptr};
     auto encode = [&](const double* values, double missing, double scale, size_t limbs, u64* dst) {
@@ -807,18 +794,14 @@ static int norm_apply(hisa_ctx* ctx, const hisa_tensor* in, const hisa_norm_plan
     if (t_analysis) TALLY(mul_scalar, HISA_OP_MUL_SCALAR, 2 * groups, l);
     if (!t_analysis) {
         ProfScope prof__("norm_times_kernel", st);
-        hipLaunchKernelGGL(norm_times_kernel, norm_grid(ctx, l, 2 * groups), dim3(NT), 0, st, ctx->d_fprimes, v.u(), scaled.u(), l, r.kw, -r.ky, log_n);
+        hipLaunchKernelGGL(norm_times_kernel, norm_grid(ctx, l, 2 * groups), dim3(NT), 0, st, ctx->d_fprimes, v.u(), scaled.u(), l, r.kw, -r.ky, r.cw, r.cy,
+                           (double)ctx->mod[l - 1], log_n);
         HIP_TRY(ctx, hipGetLastError());
     }
     TRY(rescale_fp(ctx, scaled.u(), 4 * groups, l, wy.u()));
     l -= 1;
     const int lw = l;
     const u64* w = wy.u();
-    if (!t_analysis) {
-        ProfScope prof__("norm_start_kernel", st);
-        hipLaunchKernelGGL(norm_start_kernel, norm_grid(ctx, l, 2 * groups), dim3(NT), 0, st, ctx->d_fprimes, wy.u(), l, r.cw, r.cy, log_n);
-        HIP_TRY(ctx, hipGetLastError());
-    }
     Temp pair(ctx, 2 * groups * words(2, l) * 8), y1(ctx, groups * words(2, l) * 8), y2(ctx, groups * words(2, l) * 8);
     if (!pair.ok() || !y1.ok() || !y2.ok()) return HISA_ERR_OOM;
     u64 *y = wy.u() + groups * words(2, lw), *y_next = y1.u(), *y_free = y2.u();
@@ -861,14 +844,12 @@ static int norm_apply(hisa_ctx* ctx, const hisa_tensor* in, const hisa_norm_plan
         ProductArgs g = product_base(ctx, l);
         g.n_first = (unsigned)cts;
         operand_a(g.s[0], {y, words(2, l), l}, n, per); operand_b(g.s[0], {u.u(), words(2, l), l}, n);
+        // beta q, which the division by q leaves as beta
+        g.plain_period = (unsigned)images;
+        g.s[0].add = (const u64*)p->beta->ptr; g.s[0].add_bs = words(1, l);
+        g.factor = (double)ctx->mod[l - 1];
         TRY(relinearised_products(ctx, g, cts, first.data()));
         l -= 1;
-    }
-    if (!t_analysis) {
-        ProfScope prof__("norm_shift_kernel", st);
-        hipLaunchKernelGGL(norm_shift_kernel, norm_grid(ctx, l, cts), dim3(NT), 0, st, ctx->d_fprimes, first.data(), (const u64*)p->beta->ptr,
-                           (unsigned)images, l, log_n);
-        HIP_TRY(ctx, hipGetLastError());
     }
     if (p->geom.act) {
         TRY(o.make(cts, l - 1, r.out_scale));
