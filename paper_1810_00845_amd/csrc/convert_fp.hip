@@ -1958,3 +1958,73 @@ hipError_t launch_final_inverse_rows_fp(const ConvertArgs& a, double* mid, hipSt
 #undef FINAL_CASE
     return hipGetLastError();
 }
+
+// ---- the rescale of (count x - m) gamma ----
+// As the inverse rows and the final rows of a division by the last prime, whose operand is formed on the way, in both, instead of being
+// written and read again.  Bound by memory; four waves a row at every size, as the products' rows.
+template <int K3, bool FINAL>
+__global__ __launch_bounds__(WIDE_NT, 4) void centre_rows_kernel(CentreArgs g, ConvertArgs a, int n_tasks) {
+    __shared__ double lds[WIDE_LDS];
+    const int task = wide_task(n_tasks);
+    if (task < 0) return;
+    const uint32_t t = threadIdx.x, unit = (uint32_t)task / a.n_entries, b = (uint32_t)task - unit * a.n_entries;
+    const uint32_t row = unit & ((1u << K3) - 1), e = b >> 1, poly = b & 1;
+    const int limb = FINAL ? (int)(unit >> K3) : g.limbs - 1;
+    const Modulus q = modulus(g.fprimes, limb);
+    constexpr u64 n = (u64)1 << (10 + K3);
+    const rsrc_t dst = FINAL ? make_rsrc(a.out + (u64)b * a.out_bs + (u64)limb * n + row * 1024u, 8192u)
+                             : make_rsrc(a.mid + (u64)b * n + row * 1024u, 8192u);
+    double v[4], x[4], m[4], f[4];
+    WideTwiddles w;
+    if (FINAL) {
+#pragma unroll
+        for (int r = 0; r < 4; r++) v[r] = bloadf(dst, t * 8u, (uint32_t)r * 2048u);
+    }
+    wide_twiddles(w, FINAL ? a.sfwd : a.sinv, a.table_stride, limb, row, t, q);
+    wide_load<K3>(x, g.x + (u64)e * g.x_bs + poly * g.x_ps + (u64)limb * n, 0, row, t);
+    wide_load<K3>(m, g.m + (u64)(e / g.per) * g.m_bs + poly * g.m_ps + (u64)limb * n, 0, row, t);
+    wide_load<K3>(f, g.gamma + ((u64)(e % g.period) * g.limbs + limb) * n, 0, row, t);
+    if (FINAL) wide_forward(v, COLUMNS_BOUND, w, lds, t, q, 5.2f);
+    const double count = fp_whole(g.count, q.p, q.pinv);
+    wide_from_residues(x); wide_from_residues(m); wide_from_residues(f);
+#pragma unroll
+    for (int r = 0; r < 4; r++) {      // factors canonical or normalised: products within 0.875 p
+        x[r] = fp_norm(fp_mulmod(x[r], count, q.p, q.pinv) - m[r], q.p, q.pinv);
+        x[r] = fp_norm(fp_mulmod(x[r], f[r], q.p, q.pinv), q.p, q.pinv);
+        x[r] = x[r] < 0.0 ? x[r] + q.p : x[r];
+    }
+    if (FINAL) {
+        const double pin = as_const(a.pinv_tab)[limb];
+#pragma unroll
+        for (int r = 0; r < 4; r++) v[r] = fp_mulmod(x[r] - v[r], pin, q.p, q.pinv);
+        wide_store_residues(dst, t, v, q);
+    } else {
+        wide_inverse(x, 1.0f, w, lds, t, q);
+#pragma unroll
+        for (int r = 0; r < 4; r++) bstoref(dst, t * 8u, (uint32_t)r * 2048u, x[r]);
+    }
+}
+
+template <bool FINAL>
+static hipError_t launch_centre_rows(const CentreArgs& g, const ConvertArgs& a, hipStream_t st) {
+    DRY_RUN_RETURN();
+    u64 targets = 0;
+    const u64 n = (u64)1 << a.log_n, limbs = FINAL ? a.ext_limbs : 1, tasks = (limbs * a.n_entries) << (a.log_n - 10);
+    if (a.n_entries == 0 || (a.n_entries & 1) || !convert_args_ok(a, &targets) || a.n_digits != 1 || a.dg[0].own_n || a.dg[0].out_pos0 || a.n_src != 1 ||
+        a.ext_limbs != g.limbs - 1 || a.src_pos0 != g.limbs - 1 || g.limbs > a.l || tasks > 0x7fffff00u)
+        return hipErrorInvalidValue;
+    if (!g.fprimes || !g.x || !g.m || !g.gamma || !a.mid || !a.out || !a.pinv_tab || g.per < 1 || g.period < 1 || g.x_ps < (u64)g.limbs * n ||
+        g.m_ps < (u64)g.limbs * n || a.out_bs < (u64)a.ext_limbs * n)
+        return hipErrorInvalidValue;
+    const dim3 grid((unsigned)((tasks + 7) / 8 * 8));
+    ProfScope prof__(FINAL ? "centre_rows_kernel<true>" : "centre_rows_kernel<false>", st);
+#define CENTRE_CASE(K3) case 10 + K3: hipLaunchKernelGGL((centre_rows_kernel<K3, FINAL>), grid, dim3(WIDE_NT), 0, st, g, a, (int)tasks); break
+    switch (a.log_n) {
+        CENTRE_CASE(2); CENTRE_CASE(3); CENTRE_CASE(4); CENTRE_CASE(5);
+        default: return hipErrorInvalidValue;
+    }
+#undef CENTRE_CASE
+    return hipGetLastError();
+}
+hipError_t launch_centre_inverse_rows_fp(const CentreArgs& g, const ConvertArgs& a, hipStream_t st) { return launch_centre_rows<false>(g, a, st); }
+hipError_t launch_centre_final_rows_fp(const CentreArgs& g, const ConvertArgs& a, hipStream_t st) { return launch_centre_rows<true>(g, a, st); }

@@ -2403,6 +2403,29 @@ int rescale_fp(hisa_ctx* ctx, const u64* in, size_t n_polys, int l, u64* out) {
     return rescale_core_fp(ctx, in, n_polys, l, out);
 }
 
+int centred_rescale_fp(hisa_ctx* ctx, const CentreArgs& g, size_t n_cts, u64* out) {
+    const int l = g.limbs;
+    if (l < 2) return fail(ctx, HISA_ERR_DEPTH_EXHAUSTED, "no level to rescale into");
+    if (t_analysis) {
+        TALLY(mul_plain, HISA_OP_MUL_PLAIN, n_cts, l);
+        TALLY(rescale, HISA_OP_RESCALE, n_cts, l);
+        return HISA_OK;
+    }
+    const size_t nn = ctx->N;
+    Temp y(ctx, 2 * n_cts * nn * sizeof(double));
+    if (!y.ok()) return HISA_ERR_OOM;
+    double *ones, *qlinv;
+    TRY(fp_rescale_tables(ctx, l, &ones, &qlinv));
+    ConvertArgs c = convert_base(ctx, l, 2 * n_cts);
+    c.src_pos0 = l - 1; c.n_src = 1; c.post = ones; c.mid = y.as<double>();
+    c.n_digits = 1; c.dg[0] = {ones, 0, 1, 0, 0, 0}; c.ext_limbs = l - 1; c.out = out; c.out_bs = (u64)(l - 1) * nn;
+    c.pinv_tab = qlinv;
+    HIP_TRY(ctx, launch_centre_inverse_rows_fp(g, c, ctx->stream));
+    HIP_TRY(ctx, launch_columns_fp(FP_FWD_CONV_FINAL, c, ctx->stream));
+    HIP_TRY(ctx, launch_centre_final_rows_fp(g, c, ctx->stream));
+    return HISA_OK;
+}
+
 // the same in integers
 static int rescale_core_int(hisa_ctx* ctx, const u64* in, size_t n_bp, int l, u64* out) {
     const size_t nn = ctx->N, chunk = std::min<size_t>(n_bp, 65535);

@@ -300,6 +300,16 @@ hipError_t launch_product_rows_fp(const ProductArgs& g, int log_n, hipStream_t s
 // key switches and rescale are one division
 int rotated_products_fp(hisa_ctx* ctx, const ProductArgs& g, size_t n, int32_t steps, u64* out);
 int products_rescale_fp(hisa_ctx* ctx, const ProductArgs& g, size_t n, u64* out);
+// (count x - m) gamma of ciphertexts, on `limbs` limbs: x entry e, m entry e / per, gamma plaintext [period][limbs][N] entry e % period
+struct CentreArgs {
+    const FpPrime* fprimes;
+    const u64 *x, *m, *gamma;
+    u64 x_bs, x_ps, m_bs, m_ps;
+    unsigned per, period;
+    int limbs;
+    double count;
+};
+int centred_rescale_fp(hisa_ctx* ctx, const CentreArgs& g, size_t n, u64* out);      // divided by the last prime: out [n][2][limbs - 1][N]
 // three-polynomial ciphertexts -> two polynomials at the same level: [n][3][l][N] -> out [n][2][l][N]
 int relinearize_fp(hisa_ctx* ctx, const u64* cts3, size_t n, int l, u64* out);
 int rescale_fp(hisa_ctx* ctx, const u64* in, size_t n_polys, int l, u64* out);   // [n_polys][l][N] -> [n_polys][l - 1][N]
@@ -435,6 +445,10 @@ hipError_t launch_forward_rows_fp(int mode, const ConvertArgs& a, hipStream_t st
 // FP_FWD_CONV_FINAL's rows (one digit, no addend, entries in (b, a) pairs) that go on with the inverse rows of the a polynomials: mid
 // [n_entries / 2][ext_limbs][N] is what the columns of their next key switch read
 hipError_t launch_final_inverse_rows_fp(const ConvertArgs& a, double* mid, hipStream_t st);
+// of what a CentreArgs describes: the inverse rows of its last limb (mid [2 n][N]), and the final rows of its division by that limb's
+// prime, of n ciphertexts [2][limbs - 1][N] whose columns are in a.out: the value itself is formed in both and never stored
+hipError_t launch_centre_inverse_rows_fp(const CentreArgs& g, const ConvertArgs& a, hipStream_t st);
+hipError_t launch_centre_final_rows_fp(const CentreArgs& g, const ConvertArgs& a, hipStream_t st);
 // The rows behind the columns of a key switch's digits (ConvertArgs::out: [n_entries][digits][ext_limbs][N]), with the inner
 // product with `key` and the neighbouring halves of the division that follows, for the limbs x_begin .. x_end - 1.
 // FP_INV_D_TO_Y: limbs from n_acc on are sources of that division: down [n_entries * 2][ext_limbs - n_acc][N] =

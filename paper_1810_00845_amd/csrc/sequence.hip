@@ -500,31 +500,6 @@ __global__ __launch_bounds__(NT) void norm_times_kernel(const FpPrime* fprimes, 
     out[at + (((u64)gridDim.z * limbs) << log_n)] = fp_canonical(y, p, pinv);
 }
 
-// out = (n x - m) gamma: x entry e, m entry e / per, gamma plaintext e % images, on the first `limbs` limbs
-struct CentreArgs {
-    const FpPrime* fprimes;
-    const u64 *x, *m, *gamma;
-    u64 x_bs, x_ps, m_bs, m_ps;
-    unsigned per, period;
-    int limbs;
-    u64* out;
-    double count;
-};
-__global__ __launch_bounds__(NT) void norm_centre_kernel(CentreArgs g, int log_n) {
-    const u64 n = (u64)1 << log_n, lw = (u64)g.limbs * n;
-    const int limb = blockIdx.y;
-    const u64 e = blockIdx.z, at = (u64)limb * n + (u64)blockIdx.x * NT + threadIdx.x;
-    const double p = as_const(&g.fprimes[limb].p)[0], pinv = as_const(&g.fprimes[limb].p)[1], half = as_const(&g.fprimes[limb].p)[2];
-    const double w = fp_centred_from_u64(g.gamma[(e % g.period) * lw + at], p, half), count = fp_whole(g.count, p, pinv);
-#pragma unroll
-    for (int poly = 0; poly < 2; poly++) {
-        const double x = fp_centred_from_u64(g.x[e * g.x_bs + poly * g.x_ps + at], p, half);
-        const double m = fp_centred_from_u64(g.m[(e / g.per) * g.m_bs + poly * g.m_ps + at], p, half);
-        const double d = fp_norm(fp_mulmod(x, count, p, pinv) - m, p, pinv);
-        g.out[(e * 2 + poly) * lw + at] = fp_canonical(fp_mulmod(d, w, p, pinv), p, pinv);
-    }
-}
-
 static dim3 norm_grid(const hisa_ctx* ctx, int limbs, size_t entries) { return dim3(ctx->N / NT, limbs, (unsigned)entries); }
 
 #define HISA_MAGIC_NORMPLAN 0x4e4f524du
@@ -826,17 +801,11 @@ static int norm_apply(hisa_ctx* ctx, const hisa_tensor* in, const hisa_norm_plan
         std::swap(y_next, y_free);
     }
     // (x - mean) gamma, one level above 1 / sqrt
-    Temp centred(ctx, cts * words(2, l + 1) * 8), u(ctx, cts * words(2, l) * 8);
-    if (!centred.ok() || !u.ok()) return HISA_ERR_OOM;
-    if (t_analysis) TALLY(mul_plain, HISA_OP_MUL_PLAIN, cts, l + 1);
-    if (!t_analysis) {
-        CentreArgs g = {ctx->d_fprimes, x.base, total.base, (const u64*)p->gamma->ptr, x.bs, (u64)x.limbs * n, total.bs, (u64)total.limbs * n, per,
-                        (unsigned)images, l + 1, centred.u(), r.count};
-        ProfScope prof__("norm_centre_kernel", st);
-        hipLaunchKernelGGL(norm_centre_kernel, norm_grid(ctx, l + 1, cts), dim3(NT), 0, st, g, log_n);
-        HIP_TRY(ctx, hipGetLastError());
-    }
-    TRY(rescale_fp(ctx, centred.u(), 2 * cts, l + 1, u.u()));
+    Temp u(ctx, cts * words(2, l) * 8);
+    if (!u.ok()) return HISA_ERR_OOM;
+    const CentreArgs centre = {ctx->d_fprimes, x.base, total.base, (const u64*)p->gamma->ptr, x.bs, (u64)x.limbs * n, total.bs, (u64)total.limbs * n,
+                               per, (unsigned)images, l + 1, r.count};
+    TRY(centred_rescale_fp(ctx, centre, cts, u.u()));
     Outputs o(ctx), mid(ctx);
     Outputs& first = p->geom.act ? mid : o;
     TRY(first.make(cts, l - 1, r.norm_scale));
