@@ -349,6 +349,24 @@ def test_dry_run_names_keys_and_levels():
     g.close()
 
 
+def test_dry_run_of_a_normalisation():
+    from paper_1810_00845_amd import hisa
+    g = hisa.Context(12, [50] + [BITS] * 8, 2, 50, 5)
+    like = g.tensor_encrypt(np.zeros((2, 4, 2, 3)), 2.0 ** BITS, 9)
+    plan = g.group_norm_prepare(like, None, None, 2, 1e-3, 0.1, 1.0, 2, act_ratio=0.5)
+    g.analysis_begin()
+    x = g.tensor_encrypt(np.zeros((2, 4, 2, 3)), 2.0 ** BITS, 9)
+    y = g.group_norm_apply(x, plan)
+    counts, steps = g.analysis_end()
+    assert sorted(steps) == sorted(set(g.group_norm_rot_steps(like)))
+    assert y.cts[0].limbs == counts["min_limbs"] == 9 - 8
+    # x x and its sums' product a group, three products an iteration and group, the normalised values' two; rotations of both sums
+    assert counts["relinearize"] == 4 + 4 + 2 * 3 * 4 + 2 * 8
+    assert counts["rot_left"] == 8 * len(g.group_norm_rot_steps(like))
+    g.group_norm_plan_free(plan)
+    g.close()
+
+
 def refused(code, f, *args, **kw):
     from paper_1810_00845_amd import hisa
     with pytest.raises(hisa.HisaError) as e:
