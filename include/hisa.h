@@ -560,12 +560,14 @@ int hisa_poly2_act(hisa_ctx* ctx, const hisa_tensor* in, double a, double b, his
  * modulus per level.
  * hisa_recurrence_step is one token: out = x + gates * state element by element (any width; one level, the relinearisation
  * key).  x is taken times a whole number to the scale of gates times that of state (HISA_ERR_SCALE_MISMATCH where none is
- * within 2^-16 of what that takes, here and in the other layers: scales have to be about as large as the primes).  With a state whose elements are zero but at the first token, it puts a state in front of a scan: the scan
- * of the result with the masked gates continues the sequence that ended in that state.
+ * within 2^-16 of what that takes, here and in the other layers: scales have to be about as large as the primes).  With a
+ * state whose elements are zero but at the first token, it puts a state in front of a scan: the scan of the result with the
+ * masked gates continues the sequence that ended in that state.
  * hisa_recurrence_grad is the backward pass: from the gates (masked, as above), the states h that the scan returned and the
  * gradient of those, dx = gradient of x and dgates = gradient of the gates, summed over the channels that share them (T >= 2):
  * ceil(log2 T) levels for dx and one more for dgates.  dgates is not clean and holds nothing meaningful at the first token
  * (reverse: the last), whose gate is a constant: hisa_recurrence_gates of it is the gradient of gates before their mask.
+ * dx and dgates need an array of handles each (HISA_ERR_ARG).
  * hisa_recurrence_rot_steps lists the amounts for hisa_gen_rot_mul_keys; backward != 0: those of hisa_recurrence_grad. */
 int hisa_recurrence(hisa_ctx* ctx, const hisa_tensor* gates, const hisa_tensor* x, uint32_t reverse, hisa_tensor* out);
 int hisa_recurrence_step(hisa_ctx* ctx, const hisa_tensor* gates, const hisa_tensor* state, const hisa_tensor* x,
