@@ -333,6 +333,36 @@ def test_rotation_sums_of_a_ragged_number(limbs, dnum):
     g.close()
 
 
+def test_two_contexts_at_once():
+    """Two contexts of one key and seed on streams of their own, their layers queued in turn: what one of them alone leaves."""
+    import torch
+    from paper_1810_00845_amd import hisa
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    both = []
+    for st in streams:
+        g = hisa.Context(13, [50] + [BITS] * 8, 3, 50, 5, stream=st.cuda_stream)
+        g.keygen()
+        cts = g.ct_random_batch(8, 9, 2.0 ** BITS, 21)
+        x, a = (hisa.CipherTensor(g, c, 1, len(c), 1, 7, 7, 1, 0, 1) for c in (cts[:6], cts[6:]))
+        g.gen_rot_mul_keys(g.recurrence_rot_steps(x) + g.recurrence_rot_steps(x, False, True))
+        g.gen_rot_keys(g.group_norm_rot_steps(x))
+        both.append((g, x, a, g.group_norm_prepare(x, None, None, 2, 1e-3, 0.1, 1.0, 2)))
+
+    def layers(g, x, a, plan):
+        h = g.recurrence(a, x)
+        return [h, *g.recurrence_grad(a, h, x), g.group_norm_apply(x, plan)]
+    want = [[both[0][0].ct_export(c) for c in t.cts] for t in layers(*both[0])]
+    torch.cuda.synchronize()
+    queued = [layers(*both[i % 2]) for i in range(6)]
+    for i, run in enumerate(queued):
+        for t, w in zip(run, want):
+            for c, v in zip(t.cts, w):
+                assert np.array_equal(both[i % 2][0].ct_export(c), v)
+    for g, _x, _a, plan in both:
+        g.group_norm_plan_free(plan)
+        g.close()
+
+
 # --- dry runs and refusals ---
 
 def test_dry_run_names_keys_and_levels():
