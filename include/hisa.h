@@ -551,7 +551,8 @@ int hisa_poly2_act(hisa_ctx* ctx, const hisa_tensor* in, double a, double b, his
  * Gated linear recurrence along the width of a tensor, every row (batch, channel, y) a sequence of its own:
  *     h[t] = x[t] + gates[t] h[t - 1],  h[first] = x[first];  reverse != 0: h[t] = x[t] + gates[t] h[t + 1]
  * Gates have the layout of x; x may have m times as many channels, gate ciphertext g then serves ciphertexts g m .. g m + m - 1
- * of each image (heads that share a gate; HISA_ERR_ARG where the channels do not divide so).  The gates of the first
+ * of each image (heads that share a gate; HISA_ERR_ARG where the channels do not divide so, and, for m > 1, where a last gate
+ * ciphertext holds fewer than c_inner channels: it would leave channels of x without a gate).  The gates of the first
  * token of every row (reverse: of the last) have to be encryptions of zero -- they multiply nothing, and the zero keeps the
  * rows of a ciphertext apart: hisa_recurrence_gates makes it so by one masking multiply (one level; _fixed with the mask as
  * mask_coeffs[ceil(C/c_inner)][N] at mask_scale).  A scan over T = width tokens takes ceil(log2 T) levels

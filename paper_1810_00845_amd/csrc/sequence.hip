@@ -199,6 +199,9 @@ static int check_gates(hisa_ctx* ctx, const hisa_tensor* gates, const hisa_tenso
     if (x->channels % gates->channels || t_per(x) % t_per(gates) || x->channels / gates->channels != t_per(x) / t_per(gates))
         return fail(ctx, HISA_ERR_ARG, "%u channels do not share the gates of %u", x->channels, gates->channels);
     *shared = (unsigned)(t_per(x) / t_per(gates));
+    // x's channels beside the missing ones of a part-filled gate ciphertext would have no gate
+    if (*shared > 1 && gates->channels % t_ci(gates))
+        return fail(ctx, HISA_ERR_ARG, "shared gates have to fill their ciphertexts: %u channels, %u to a ciphertext", gates->channels, t_ci(gates));
     if (t_ncts(x) > 16384) return fail(ctx, HISA_ERR_ARG, "%zu ciphertexts in one call", t_ncts(x));
     return HISA_OK;
 }
