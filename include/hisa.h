@@ -585,8 +585,8 @@ int hisa_recurrence_rot_steps(hisa_ctx* ctx, const hisa_tensor* like, uint32_t r
  *     y = gamma[c] (x - mean) / sqrt(var + eps) + beta[c],   var = mean of (x - mean)^2;   act = 1: y^2 + act_ratio y
  * (a y^2 + b y is a times the latter with act_ratio = b / a; the factor belongs in the next layer's weights, as with
  * hisa_poly2_act).  HW- and CHW-tiled tensors, channels last among them (c_stride = 1, w_stride = c_inner); a ciphertext
- * may hold channels of one group only (HISA_ERR_ARG).  groups = 1 is a layer norm of the whole image, groups = channels an
- * instance norm.
+ * may hold channels of one group only (HISA_ERR_ARG).  groups = 1 is a layer norm of the whole image (its last ciphertext may
+ * hold fewer than c_inner channels), groups = channels an instance norm.
  * 1 / sqrt is a line and `iterations` odd cubics, y <- c1 y - c3 v y^3, each the one that stays nearest to its target on
  * what the step before leaves of [var_lo, var_hi]: var + eps has to lie in there (above it the result is nothing, below it
  * falls short).  The largest relative error of 1 / sqrt for var_hi / var_lo = 16 is 7e-2, 4e-3, 1e-5, 7e-11 with 1, 2, 3, 4

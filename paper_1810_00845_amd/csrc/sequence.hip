@@ -618,7 +618,7 @@ static int check_norm(hisa_ctx* ctx, const hisa_tensor* t, const hisa_norm_geom*
     TRY(check_scales(ctx, t));
     TRY(need_fused(ctx, "a normalisation"));
     TRY(check_clean(ctx, t, "inputs of a normalisation"));
-    if (!g || g->groups == 0 || t->channels % g->groups || (t->channels / g->groups) % t_ci(t))
+    if (!g || g->groups == 0 || t->channels % g->groups || (g->groups > 1 && (t->channels / g->groups) % t_ci(t)))
         return fail(ctx, HISA_ERR_ARG, "%u channels, %u to a ciphertext: no ciphertext may hold channels of two groups", t->channels, t_ci(t));
     if (g->iterations < 1 || g->iterations > 16 || g->act > 1) return fail(ctx, HISA_ERR_ARG, "iterations 1 to 16, act 0 or 1");
     if (!(g->eps >= 0.0) || !(g->var_lo > 0.0) || !(g->var_hi > g->var_lo) || !isfinite(g->var_hi) || !(g->eps <= g->var_hi) || (g->act && !isfinite(g->act_ratio)))
@@ -660,7 +660,7 @@ static int norm_prepare(hisa_ctx* ctx, const hisa_tensor* like, const double* ga
     auto encode = [&](const double* values, double missing, double scale, size_t limbs, u64* dst) {
         std::vector<double> v((size_t)per * ci * hw);
         for (size_t c = 0; c < (size_t)per * ci; c++) {
-            const double x = values ? values[c] : missing;
+            const double x = c >= like->channels ? 0.0 : values ? values[c] : missing;      // beside a part-filled last ciphertext's
             if (!(fabs(x) * scale < 4.6e18)) return fail(ctx, HISA_ERR_ARG, "a factor or bias times its scale does not fit 63 bits");
             std::fill(v.begin() + c * hw, v.begin() + (c + 1) * hw, x);
         }

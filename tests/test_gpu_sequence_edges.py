@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 
 import sequence_plain as plain
-from test_gpu_sequence import BITS, limit, refused
+from test_gpu_sequence import BITS, limit, pair, random_tensors, refused, same
 
 pytestmark = pytest.mark.gpu
 ARG = -1
@@ -51,4 +51,46 @@ def test_part_filled_and_shared_values(c_inner, gates, channels):
     assert np.abs(g.tensor_decrypt(dx) - wx).max() <= tol
     # products of states and gradients below ten each, summed over the sharers
     assert np.abs(g.tensor_decrypt(g.recurrence_gates(dg)) - wa).max() <= tol * 20 * (channels // gates)
+    g.close()
+
+
+# --- a group that ends in a part-filled ciphertext ---
+
+def test_one_group_in_a_part_filled_ciphertext_bits():
+    from oracle import sequence as seq
+    from paper_1810_00845_amd import synth
+    g, o = pair(12, 7, 3)
+    gt, ot = random_tensors(g, o, 4, 7, 2.0 ** BITS, 3, batch=2, channels=7, height=2, width=3, c_inner=4, c_stride=16)
+    steps = g.group_norm_rot_steps(gt)
+    g.gen_rot_keys(steps); o.gen_rot_keys(steps)
+    gamma, beta = (np.stack([synth.plaintext_coeffs(k + i, g.N, bits) for i in range(2)]) for k, bits in ((7, 30), (70, 40)))
+    args = (1, 1e-3, 0.05, 2.0, 1)
+    plan = g.group_norm_prepare_fixed(gt, gamma, 2.0 ** 35, beta, *args, act_ratio=0.5)
+    same(g, o, g.group_norm_apply(gt, plan), seq.group_norm_fixed(o, ot, gamma, 2.0 ** 35, beta, *args, 0.5))
+    g.group_norm_plan_free(plan)
+    g.close()
+
+
+@pytest.mark.parametrize("shape,layout", [((2, 5, 3, 4), dict(c_inner=4, c_stride=1, w_stride=4)), ((1, 3, 3, 3), dict(c_inner=8, c_stride=16))])
+def test_one_group_in_a_part_filled_ciphertext_values(shape, layout):
+    from paper_1810_00845_amd import hisa
+    rng = np.random.default_rng(shape[1])
+    x = rng.normal(0.3, 0.8, shape)
+    gamma, beta = rng.uniform(0.5, 1.5, shape[1]), rng.uniform(-1, 1, shape[1])
+    var = x.reshape(shape[0], -1).var(-1)
+    lo, hi = var.min() / 2, var.max() * 2
+    g = hisa.Context(13, [50] + [BITS] * 12, 3, 50, 7)
+    g.keygen()
+    t = g.tensor_encrypt(x, 2.0 ** BITS, 13, **layout)
+    g.gen_rot_keys(g.group_norm_rot_steps(t))
+    # as test_group_norm_values: the cubics' error, and noise at 1 / 64 of the scale over twelve divisions
+    tol = np.abs(x).max() / np.sqrt(lo) * 1.5 * plain.cubic_error(lo, hi, 4) + limit(13, g.K, 64 * 12, np.abs(x).max() / np.sqrt(lo) * 1.5 / lo)
+    for ga, be in ((gamma, beta), (None, None)):
+        plan = g.group_norm_prepare(t, ga, be, 1, 1e-3, lo, hi, 4)
+        y = g.group_norm_apply(t, plan)
+        want = plain.group_norm(x, *((np.ones(shape[1]), np.zeros(shape[1])) if ga is None else (ga, be)), 1, 1e-3)
+        assert y.clean and np.abs(g.tensor_decrypt(y) - want).max() <= tol
+        # the slots of the missing channels hold zeros
+        assert np.abs(g.tensor_decrypt(y.shaped_like(channels=len(y.cts) // shape[0] * layout["c_inner"]))[:, shape[1]:]).max() <= tol
+        g.group_norm_plan_free(plan)
     g.close()
