@@ -89,6 +89,12 @@ static int check_scales(hisa_ctx* ctx, const hisa_tensor* t) {
     return HISA_OK;
 }
 
+// whether the elements of a ciphertext lie in the same slots: the stride of an extent of one says nothing
+static bool same_slots(const hisa_tensor& a, const hisa_tensor& b) {
+    return a.height == b.height && a.width == b.width && a.offset == b.offset && t_ci(&a) == t_ci(&b) &&
+           (a.height == 1 || a.h_stride == b.h_stride) && (a.width == 1 || a.w_stride == b.w_stride) && (t_ci(&a) == 1 || a.c_stride == b.c_stride);
+}
+
 // round(v), ties away from zero, as the whole number that stands for a factor.  Scales as small as the primes of a
 // parameter set leave such factors 25 bits and more; one that is off by more than 2^-16 says that the scales do not fit the primes.
 static int whole_factor(hisa_ctx* ctx, double v, double* out) {
@@ -192,10 +198,7 @@ static int check_gates(hisa_ctx* ctx, const hisa_tensor* gates, const hisa_tenso
     TRY(check_tensor(ctx, x));
     TRY(check_scales(ctx, gates));
     TRY(check_scales(ctx, x));
-    const bool same = gates->batch == x->batch && gates->height == x->height && gates->width == x->width && gates->offset == x->offset &&
-                      (x->height == 1 || gates->h_stride == x->h_stride) && (x->width == 1 || gates->w_stride == x->w_stride) &&
-                      t_ci(gates) == t_ci(x) && (t_ci(x) == 1 || gates->c_stride == x->c_stride);
-    if (!same) return fail(ctx, HISA_ERR_ARG, "gates and inputs have different layouts");
+    if (gates->batch != x->batch || !same_slots(*gates, *x)) return fail(ctx, HISA_ERR_ARG, "gates and inputs have different layouts");
     if (x->channels % gates->channels || t_per(x) % t_per(gates) || x->channels / gates->channels != t_per(x) / t_per(gates))
         return fail(ctx, HISA_ERR_ARG, "%u channels do not share the gates of %u", x->channels, gates->channels);
     *shared = (unsigned)(t_per(x) / t_per(gates));
@@ -508,7 +511,8 @@ static dim3 norm_grid(const hisa_ctx* ctx, int limbs, size_t entries) { return d
 #define HISA_MAGIC_NORMPLAN 0x4e4f524du
 struct hisa_norm_plan {
     uint32_t magic;
-    uint32_t channels, height, width, h_stride, w_stride, offset, c_inner, c_stride, limbs;
+    hisa_tensor like;            // its layout, without handles
+    uint32_t limbs;
     double scale;
     hisa_norm_geom geom;
     double gamma_scale;
@@ -655,8 +659,8 @@ static int norm_prepare(hisa_ctx* ctx, const hisa_tensor* like, const double* ga
     TRY(norm_schedule(ctx, *geom, n, level, s, gamma_scale, &full));
     const uint32_t ci = t_ci(like), per = (uint32_t)t_per(like);
     const size_t hw = (size_t)like->height * like->width, lg = (size_t)full.level_y + 1, lb = (size_t)full.level_y;
-    hisa_norm_plan* p = new hisa_norm_plan{HISA_MAGIC_NORMPLAN, like->channels, like->height, like->width, like->h_stride, like->w_stride, like->offset,
-                                           ci, like->c_stride, (uint32_t)level, s, *geom, gamma_scale, nullptr, nullptr};
+    hisa_norm_plan* p = new hisa_norm_plan{HISA_MAGIC_NORMPLAN, *like, (uint32_t)level, s, *geom, gamma_scale, nullptr, nullptr};
+    p->like.cts = nullptr;
     auto encode = [&](const double* values, double missing, double scale, size_t limbs, u64* dst) {
         std::vector<double> v((size_t)per * ci * hw);
         for (size_t c = 0; c < (size_t)per * ci; c++) {
@@ -709,8 +713,7 @@ static int norm_apply(hisa_ctx* ctx, const hisa_tensor* in, const hisa_norm_plan
     if (!ctx) return HISA_ERR_ARG;
     if (!p || p->magic != HISA_MAGIC_NORMPLAN || !out || !out->cts) return fail(ctx, HISA_ERR_ARG, "bad argument");
     TRY(check_norm(ctx, in, &p->geom));
-    if (in->channels != p->channels || in->height != p->height || in->width != p->width || in->h_stride != p->h_stride || in->w_stride != p->w_stride ||
-        in->offset != p->offset || t_ci(in) != p->c_inner || in->c_stride != p->c_stride)
+    if (in->channels != p->like.channels || !same_slots(*in, p->like))
         return fail(ctx, HISA_ERR_ARG, "the plan was prepared for another layout");
     if (in->cts[0]->limbs != p->limbs) return fail(ctx, HISA_ERR_LEVEL_MISMATCH, "the plan was prepared for %u limbs", p->limbs);
     if (fabs(in->cts[0]->scale - p->scale) > ldexp(p->scale, -30)) return fail(ctx, HISA_ERR_SCALE_MISMATCH, "the plan was prepared for scale %g", p->scale);

@@ -94,3 +94,29 @@ def test_one_group_in_a_part_filled_ciphertext_values(shape, layout):
         assert np.abs(g.tensor_decrypt(y.shaped_like(channels=len(y.cts) // shape[0] * layout["c_inner"]))[:, shape[1]:]).max() <= tol
         g.group_norm_plan_free(plan)
     g.close()
+
+
+# --- plans and layouts ---
+
+@pytest.mark.parametrize("shape,other", [((1, 2, 3, 4), dict(c_stride=7)), ((1, 2, 1, 4), dict(h_stride=9)), ((1, 2, 3, 1), dict(w_stride=5)),
+                                         ((1, 2, 1, 1), dict(h_stride=9, w_stride=5, c_stride=3))])
+def test_a_plan_does_not_ask_for_strides_of_single_elements(shape, other):
+    """Strides of an extent of one place nothing: the same slots, the same plan, the same bits."""
+    from paper_1810_00845_amd import hisa
+    g = hisa.Context(12, [50] + [BITS] * 6, 2, 50, 5)
+    g.keygen()
+    t = g.tensor_encrypt(np.random.default_rng(1).normal(size=shape), 2.0 ** BITS, 7)
+    g.gen_rot_keys(g.group_norm_rot_steps(t) or [0])
+    plan = g.group_norm_prepare(t, None, None, 1, 1e-3, 0.1, 4.0, 1)
+    want = g.group_norm_apply(t, plan)
+    moved = t.shaped_like(**other)
+    assert g.group_norm_rot_steps(moved) == g.group_norm_rot_steps(t)
+    for a, b in zip(want.cts, g.group_norm_apply(moved, plan).cts):
+        assert np.array_equal(g.ct_export(a), g.ct_export(b))
+    for wrong in (dict(offset=1), dict(height=shape[2] + 1), dict(width=shape[3] + 1)):
+        refused(ARG, g.group_norm_apply, t.shaped_like(**wrong), plan)
+    if shape[2] > 1 and shape[3] > 1:
+        refused(ARG, g.group_norm_apply, t.shaped_like(h_stride=t.h_stride + 1), plan)
+        refused(ARG, g.group_norm_apply, t.shaped_like(w_stride=2, h_stride=8), plan)
+    g.group_norm_plan_free(plan)
+    g.close()
