@@ -659,7 +659,9 @@ static int norm_prepare(hisa_ctx* ctx, const hisa_tensor* like, const double* ga
     TRY(norm_schedule(ctx, *geom, n, level, s, gamma_scale, &full));
     const uint32_t ci = t_ci(like), per = (uint32_t)t_per(like);
     const size_t hw = (size_t)like->height * like->width, lg = (size_t)full.level_y + 1, lb = (size_t)full.level_y;
-    hisa_norm_plan* p = new hisa_norm_plan{HISA_MAGIC_NORMPLAN, *like, (uint32_t)level, s, *geom, gamma_scale, nullptr, nullptr};
+    auto free_plan = [&](hisa_norm_plan* q) { norm_plan_free(ctx, q); };       // also where the host has no memory to encode from
+    std::unique_ptr<hisa_norm_plan, decltype(free_plan)> p(
+        new hisa_norm_plan{HISA_MAGIC_NORMPLAN, *like, (uint32_t)level, s, *geom, gamma_scale, nullptr, nullptr}, free_plan);
     p->like.cts = nullptr;
     auto encode = [&](const double* values, double missing, double scale, size_t limbs, u64* dst) {
         std::vector<double> v((size_t)per * ci * hw);
@@ -670,19 +672,13 @@ static int norm_prepare(hisa_ctx* ctx, const hisa_tensor* like, const double* ga
         }
         return encode_sparse_batch(ctx, tensor_slots(like), v.data(), per, scale, (int)limbs, dst);
     };
-    int rc = HISA_OK;
     p->gamma = dev_alloc(ctx, (size_t)per * lg * ctx->N * sizeof(u64));
     p->beta = p->gamma ? dev_alloc(ctx, (size_t)per * lb * ctx->N * sizeof(u64)) : nullptr;
-    if (!p->beta) rc = HISA_ERR_OOM;
-    if (rc == HISA_OK)
-        rc = gamma_coeffs ? coeffs_to_plain_batch(ctx, gamma_coeffs, per, (int)lg, (u64*)p->gamma->ptr) : encode(gamma, 1.0, gamma_scale, lg, (u64*)p->gamma->ptr);
-    if (rc == HISA_OK)
-        rc = beta_coeffs ? coeffs_to_plain_batch(ctx, beta_coeffs, per, (int)lb, (u64*)p->beta->ptr) : encode(beta, 0.0, full.norm_scale, lb, (u64*)p->beta->ptr);
-    if (rc != HISA_OK) {
-        norm_plan_free(ctx, p);
-        return rc;
-    }
-    *out = p;
+    if (!p->beta) return HISA_ERR_OOM;
+    u64 *g = (u64*)p->gamma->ptr, *b = (u64*)p->beta->ptr;
+    TRY(gamma_coeffs ? coeffs_to_plain_batch(ctx, gamma_coeffs, per, (int)lg, g) : encode(gamma, 1.0, gamma_scale, lg, g));
+    TRY(beta_coeffs ? coeffs_to_plain_batch(ctx, beta_coeffs, per, (int)lb, b) : encode(beta, 0.0, full.norm_scale, lb, b));
+    *out = p.release();
     return HISA_OK;
 }
 

@@ -1,0 +1,87 @@
+"""GPU: a host allocation that fails inside a call of the sequence layers is HISA_ERR_OOM, takes nothing with it and leaves the context
+usable.  A child process of its own loads an operator new that throws where it is told to, in calls from libhisa.so only."""
+import os
+import subprocess
+import sys
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+HOOK = r'''
+#include <dlfcn.h>
+#include <cstdlib>
+#include <cstring>
+#include <new>
+static thread_local long countdown = -1, seen = 0;
+static thread_local std::size_t at_least = 0;
+extern "C" void arm(long n, std::size_t bytes) { countdown = n; at_least = bytes; seen = 0; }   // the n-th (from 0) of that size and more
+extern "C" long disarm() { countdown = -1; return seen; }
+static void* get(std::size_t n, void* from) {
+    Dl_info at;
+    if (countdown >= 0 && n >= at_least && dladdr(from, &at) && std::strstr(at.dli_fname, "libhisa")) {
+        seen++;
+        if (countdown-- == 0) throw std::bad_alloc();
+    }
+    void* p = std::malloc(n ? n : 1);
+    if (!p) throw std::bad_alloc();
+    return p;
+}
+void* operator new(std::size_t n) { return get(n, __builtin_return_address(0)); }
+void* operator new[](std::size_t n) { return get(n, __builtin_return_address(0)); }
+'''
+
+START = r'''
+import ctypes as C, sys
+import numpy as np, torch
+hook = C.CDLL(sys.argv[1], mode=C.RTLD_GLOBAL)
+hook.arm.argtypes = [C.c_long, C.c_size_t]
+hook.disarm.restype = C.c_long
+from paper_1810_00845_amd import hisa
+
+def failing(n, f, *args, at_least=0, **kw):
+    """f with the n-th allocation refused: whether one was, and what f returned."""
+    hook.arm(n, at_least)
+    try:
+        r = f(*args, **kw)
+    except hisa.HisaError as e:
+        assert hook.disarm() == n + 1 and e.code == -7, (n, e)
+        return True, None
+    assert hook.disarm() <= n
+    return False, r
+
+def free_memory():
+    torch.cuda.synchronize()
+    return torch.cuda.mem_get_info()[0]
+'''
+
+
+@pytest.fixture(scope="module")
+def hook(tmp_path_factory):
+    d = tmp_path_factory.mktemp("hook")
+    src, lib = d / "hook.cpp", d / "hook.so"
+    src.write_text(HOOK)
+    subprocess.check_call(["g++", "-O1", "-shared", "-fPIC", "-fno-optimize-sibling-calls", "-o", str(lib), str(src), "-ldl"])
+    return str(lib)
+
+
+def child(hook, body):
+    r = subprocess.run([sys.executable, "-c", START + body + "\nprint('child done')", hook], cwd=ROOT, capture_output=True, text=True, timeout=100)
+    assert r.returncode == 0 and r.stdout.endswith("child done\n"), (r.returncode, r.stdout[-2000:], r.stderr[-4000:])
+
+
+def test_a_plan_that_cannot_be_encoded_leaves_no_device_memory(hook):
+    child(hook, r'''
+g = hisa.Context(13, [50] + [40] * 8, 3, 50, 7)
+t = g.tensor_encrypt(np.zeros((1, 16, 30, 30)), 2.0 ** 40, 9)
+args = (t, np.ones(16), np.zeros(16), 2, 1e-3, 0.1, 4.0, 2)
+plan = g.group_norm_prepare(*args)
+g.group_norm_plan_free(plan)
+before = free_memory()
+for i in range(24):      # gamma's values for all slots, beta's: 16 900 8 bytes each, behind both device blocks (4 and 3 MB)
+    assert failing(i % 2, g.group_norm_prepare, *args, at_least=100000)[0]
+assert before - free_memory() < 8 << 20, before - free_memory()
+g.group_norm_plan_free(g.group_norm_prepare(*args))
+g.close()
+''')
