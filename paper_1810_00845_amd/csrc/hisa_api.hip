@@ -8,6 +8,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <memory>
 
 #include "hisa_internal.hpp"
 
@@ -208,9 +209,15 @@ DevBlock* dev_alloc(hisa_ctx* ctx, size_t bytes) {
         }
         ctx->pool_bytes += bytes;
     }
-    DevBlock* b = new DevBlock{p, bytes, 1};
-    ctx->live[(uintptr_t)p] = bytes;
-    return b;
+    try {
+        std::unique_ptr<DevBlock> b(new DevBlock{p, bytes, 1});
+        ctx->live[(uintptr_t)p] = bytes;
+        return b.release();
+    } catch (...) {      // no host memory to keep account of it with
+        (void)hipFree(p);
+        fail(ctx, HISA_ERR_OOM, "no host memory");
+        return nullptr;
+    }
 }
 
 u64 dev_words_behind(const hisa_ctx* ctx, const void* p) {
@@ -228,7 +235,11 @@ void dev_release(hisa_ctx* ctx, DevBlock* b) {
     if (!b) return;
     if (--b->refs > 0) return;
     ctx->live.erase((uintptr_t)b->ptr);
-    ctx->pool[b->bytes].push_back(b->ptr);
+    try {
+        ctx->pool[b->bytes].push_back(b->ptr);
+    } catch (...) {      // destructors come here: nothing may be thrown (hipFree waits for what is queued)
+        (void)hipFree(b->ptr);
+    }
     delete b;
 }
 
@@ -260,8 +271,15 @@ int alloc_ct_batch(hisa_ctx* ctx, size_t n, uint32_t polys, uint32_t limbs, doub
     DevBlock* blk = dev_alloc(ctx, n * words * sizeof(u64));
     if (!blk) return HISA_ERR_OOM;
     blk->refs = (int)n;
-    for (size_t i = 0; i < n; i++)
-        out[i] = new hisa_ct{HISA_MAGIC_CT, blk, (u64*)blk->ptr + i * words, polys, limbs, scale};
+    size_t i = 0;
+    try {
+        for (; i < n; i++) out[i] = new hisa_ct{HISA_MAGIC_CT, blk, (u64*)blk->ptr + i * words, polys, limbs, scale};
+    } catch (...) {
+        while (i) { delete out[--i]; out[i] = nullptr; }
+        blk->refs = 1;
+        dev_release(ctx, blk);
+        return fail(ctx, HISA_ERR_OOM, "no host memory");
+    }
     if (t_analysis && n && (t_analysis->c.min_limbs == 0 || limbs < t_analysis->c.min_limbs)) t_analysis->c.min_limbs = limbs;
     return HISA_OK;
 }

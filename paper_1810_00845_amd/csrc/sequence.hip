@@ -5,7 +5,6 @@
 
 #include <algorithm>
 #include <memory>
-#include <new>
 
 #include "fp_device.hpp"
 
@@ -179,13 +178,14 @@ static int relinearised_products(hisa_ctx* ctx, const ProductArgs& g, size_t ent
     });
 }
 
-// Nothing throws across the C boundary: what the host containers may throw becomes an error code.
+// Nothing throws across the C boundary: what the host containers may throw (std::bad_alloc, std::length_error) becomes an error code.
+// The message needs no memory of its own: a std::string keeps 15 characters.
 template <class F>
 static int guarded(hisa_ctx* ctx, F body) {
     try {
         return body();
-    } catch (const std::bad_alloc&) {
-        return fail(ctx, HISA_ERR_OOM, "out of host memory");
+    } catch (...) {
+        return fail(ctx, HISA_ERR_OOM, "no host memory");
     }
 }
 
@@ -445,9 +445,11 @@ static int recurrence_gates(hisa_ctx* ctx, const hisa_tensor* gates, bool revers
                 for (size_t k = 0; k < hw; k++) ones[((size_t)j * ci + c) * hw + k] = k % w == (reverse ? w - 1 : 0) ? 0.0 : 1.0;
         if (!t_analysis) TRY(encode_sparse_batch(ctx, tensor_slots(gates), ones.data(), per, scale, (int)l, masks.u()));
     }
-    std::vector<hisa_ct*> xs;
-    TRY(mask_run(ctx, gates, masks.u(), scale, xs));
-    return mask_finish(ctx, gates, xs, out);
+    Outputs o(ctx);
+    TRY(mask_run(ctx, gates, masks.u(), scale, o.v));
+    TRY(mask_finish(ctx, gates, o.v, out));
+    o.v.clear();
+    return HISA_OK;
 }
 
 extern "C" int hisa_recurrence_gates(hisa_ctx* ctx, const hisa_tensor* gates, uint32_t reverse, hisa_tensor* out) {

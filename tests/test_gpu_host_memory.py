@@ -85,3 +85,42 @@ assert before - free_memory() < 8 << 20, before - free_memory()
 g.group_norm_plan_free(g.group_norm_prepare(*args))
 g.close()
 ''')
+
+
+def test_any_allocation_of_a_layer_may_fail(hook):
+    """The first allocation of a call refused, then its second, and so on until none is left to refuse."""
+    child(hook, r'''
+g = hisa.Context(12, [50] + [40] * 7, 2, 50, 7)
+g.keygen()
+
+def tensor(n, counter):
+    cts = g.ct_random_batch(n, 8, 2.0 ** 40, counter)
+    return hisa.CipherTensor(g, [g.copy(c) for c in cts], 1, n, 1, 5, 5, 1, 0, 1)       # an allocation each: calls gather them
+a, x, h = tensor(2, 1), tensor(4, 100), tensor(4, 200)
+g.gen_rot_mul_keys(g.recurrence_rot_steps(x) + g.recurrence_rot_steps(x, False, True))
+g.gen_rot_keys(g.group_norm_rot_steps(x))
+norm = (None, None, 2, 1e-3, 0.1, 1.0, 1)
+plan = g.group_norm_prepare(x, *norm, act_ratio=0.5)
+calls = [lambda: (g.recurrence(a, x),), lambda: (g.recurrence_step(a, h, x),), lambda: g.recurrence_grad(a, h, x),
+         lambda: (g.recurrence_gates(a),), lambda: (g.group_norm_apply(x, plan),), lambda: (g.recurrence_rot_steps(x),),
+         lambda: (g.group_norm_rot_steps(x),), lambda: (g.group_norm_plan_free(g.group_norm_prepare(x, *norm)),)]
+
+def bits(out):
+    return [g.ct_export(c) if isinstance(t, hisa.CipherTensor) else t for t in out for c in (t.cts if isinstance(t, hisa.CipherTensor) else [0])]
+want = [bits(f()) for f in calls]       # and every block that a call takes is in the pool
+before = free_memory()
+for k, (f, w) in enumerate(zip(calls, want)):
+    n = 0
+    while True:
+        refused, out = failing(n, f)
+        if not refused:
+            break
+        n += 1
+    print("call", k, "allocations", n, "device bytes", before - free_memory(), flush=True)
+    assert n > 0 and all(np.array_equal(p, q) for p, q in zip(bits(out), w))
+    out = None
+# a ciphertext is 512 KB, and a call holds dozens of them: one lost by every refusal would be gigabytes
+assert before - free_memory() <= 8 << 20, before - free_memory()
+g.group_norm_plan_free(plan)
+g.close()
+''')
