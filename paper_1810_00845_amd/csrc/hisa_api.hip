@@ -754,21 +754,32 @@ static int fill_switch_key(hisa_ctx* ctx, u64 key_id, const u64* target, const S
     return HISA_OK;
 }
 
-// The key is registered only once every launch that builds it has been queued: a failure on the way (no memory for
-// the temporary, a refused launch) frees the block and leaves no half-built key behind for later calls to trust.
-static int gen_switch_key(hisa_ctx* ctx, u64 key_id, const u64* target) {
-    const size_t words = (size_t)ctx->dnum * 2 * ctx->total * ctx->N;
+// Device memory of a key in the making.  It is registered only once every launch that builds it has been queued: a failure on
+// the way (no memory on either side, a refused launch) frees the block and leaves no half-built key behind for later calls to trust.
+struct NewKey {
+    hisa_ctx* ctx;
+    size_t words;
     void* p = nullptr;
-    HIP_TRY(ctx, hipMalloc(&p, words * sizeof(u64)));
-    SwitchKey key{nullptr, (u64*)p};
-    const int rc = fill_switch_key(ctx, key_id, target, key);
-    if (rc != HISA_OK) {
+    explicit NewKey(hisa_ctx* c) : ctx(c), words((size_t)c->dnum * 2 * c->total * c->N) {}
+    ~NewKey() {
+        if (!p) return;
         (void)hipStreamSynchronize(ctx->stream);   // nothing queued may still write to the block
         (void)hipFree(p);
-        return rc;
     }
-    key.blk = new DevBlock{p, words * sizeof(u64), 1};
-    ctx->keys[key_id] = key;
+    void enter(u64 key_id) {
+        std::unique_ptr<DevBlock> blk(new DevBlock{p, words * sizeof(u64), 1});
+        ctx->keys[key_id] = SwitchKey{blk.get(), (u64*)p};
+        blk.release();
+        p = nullptr;
+    }
+    NewKey(const NewKey&) = delete;
+    NewKey& operator=(const NewKey&) = delete;
+};
+static int gen_switch_key(hisa_ctx* ctx, u64 key_id, const u64* target) {
+    NewKey made(ctx);
+    HIP_TRY(ctx, hipMalloc(&made.p, made.words * sizeof(u64)));
+    TRY(fill_switch_key(ctx, key_id, target, SwitchKey{nullptr, (u64*)made.p}));
+    made.enter(key_id);
     return HISA_OK;
 }
 
@@ -813,8 +824,7 @@ extern "C" int hisa_gen_rot_keys(hisa_ctx* ctx, const int32_t* left_steps, size_
     return HISA_OK;
 }
 
-extern "C" int hisa_gen_rot_mul_keys(hisa_ctx* ctx, const int32_t* left_steps, size_t count) {
-    if (!ctx) return HISA_ERR_ARG;
+static int gen_rot_mul_keys(hisa_ctx* ctx, const int32_t* left_steps, size_t count) {
     if (!fused_key_switch_available(ctx)) return fail(ctx, HISA_ERR_ARG, "products of rotated ciphertexts need " FUSED_PATH);
     TRY(hisa_gen_rot_keys(ctx, left_steps, count));
     for (size_t i = 0; i < count; i++) {
@@ -827,6 +837,11 @@ extern "C" int hisa_gen_rot_mul_keys(hisa_ctx* ctx, const int32_t* left_steps, s
         TRY(gen_switch_key(ctx, product_key_id(g), tgt.u()));
     }
     return HISA_OK;
+}
+
+extern "C" int hisa_gen_rot_mul_keys(hisa_ctx* ctx, const int32_t* left_steps, size_t count) {
+    if (!ctx) return HISA_ERR_ARG;
+    return guarded(ctx, [&] { return gen_rot_mul_keys(ctx, left_steps, count); });
 }
 
 // ---------------------------------------------------------------------------
@@ -2598,35 +2613,40 @@ extern "C" int hisa_key_export(hisa_ctx* ctx, uint64_t key_id, uint64_t* host) {
     return HISA_OK;
 }
 
-extern "C" int hisa_key_import(hisa_ctx* ctx, uint64_t key_id, const uint64_t* host) {
-    if (!ctx || !host) return fail(ctx, HISA_ERR_ARG, "bad argument");
+static int key_import(hisa_ctx* ctx, u64 key_id, const uint64_t* host) {
     if (t_analysis) return fail(ctx, HISA_ERR_ARG, "keys cannot be imported during an analysis (no kernel runs)");
     const u64 g = key_id & 0xffffffffu, kind = key_id >> 32;
     const bool galois = (g & 1) && g > 1 && g < 2 * (u64)ctx->N;
     if (!(key_id == 0 || (kind <= 1 && galois))) return fail(ctx, HISA_ERR_ARG, "%llu names no key", (unsigned long long)key_id);
-    const size_t n = ctx->N, rows = (size_t)ctx->dnum * 2 * ctx->total, words = rows * n;
+    const size_t n = ctx->N, rows = (size_t)ctx->dnum * 2 * ctx->total;
     for (size_t r = 0; r < rows; r++)
         for (size_t j = 0; j < n; j++)
             if (host[r * n + j] >= ctx->mod[r % ctx->total]) return fail(ctx, HISA_ERR_ARG, "a value of the key is no residue of its prime");
+    NewKey made(ctx);
     auto it = ctx->keys.find(key_id);
-    u64* data = it == ctx->keys.end() ? nullptr : it->second.data;
-    if (!data) {
-        void* p = nullptr;
-        HIP_TRY(ctx, hipMalloc(&p, words * sizeof(u64)));
-        data = (u64*)p;
-    }
-    hipError_t e = hipMemcpyAsync(data, host, words * sizeof(u64), hipMemcpyHostToDevice, ctx->stream);
+    const bool there = it != ctx->keys.end();
+    if (!there) HIP_TRY(ctx, hipMalloc(&made.p, made.words * sizeof(u64)));
+    u64* data = there ? it->second.data : (u64*)made.p;
+    hipError_t e = hipMemcpyAsync(data, host, made.words * sizeof(u64), hipMemcpyHostToDevice, ctx->stream);
     if (e == hipSuccess && fused_key_switch_available(ctx))
         e = launch_key_to_doubles(ctx->d_fprimes, data, (int)ctx->dnum * 2, (int)ctx->total, (int)ctx->log_n, ctx->stream);
     const hipError_t waited = hipStreamSynchronize(ctx->stream);       // the caller's array may go
     if (e == hipSuccess) e = waited;
     if (e != hipSuccess) {       // nothing half written is left behind
-        if (it != ctx->keys.end()) { delete it->second.blk; ctx->keys.erase(it); }
-        (void)hipFree(data);
+        if (there) {
+            (void)hipFree(data);
+            delete it->second.blk;
+            ctx->keys.erase(it);
+        }
         return fail(ctx, HISA_ERR_HIP, "key import: %s", hipGetErrorString(e));
     }
-    if (it == ctx->keys.end()) ctx->keys[key_id] = SwitchKey{new DevBlock{data, words * sizeof(u64), 1}, data};
+    if (!there) made.enter(key_id);
     return HISA_OK;
+}
+
+extern "C" int hisa_key_import(hisa_ctx* ctx, uint64_t key_id, const uint64_t* host) {
+    if (!ctx || !host) return fail(ctx, HISA_ERR_ARG, "bad argument");
+    return guarded(ctx, [&] { return key_import(ctx, key_id, host); });
 }
 
 extern "C" int hisa_secret_export(hisa_ctx* ctx, int64_t* host_coeffs) {

@@ -140,6 +140,17 @@ struct hisa_ctx {
 // ---- host helpers shared by hisa_api.hip and layers.hip ----
 int fail(hisa_ctx* ctx, int code, const char* fmt, ...);
 
+// Nothing throws across the C boundary: what the host containers may throw (std::bad_alloc, std::length_error) becomes an error code.
+// The message needs no memory of its own: a std::string keeps 15 characters.
+template <class F>
+int guarded(hisa_ctx* ctx, F body) {
+    try {
+        return body();
+    } catch (...) {
+        return fail(ctx, HISA_ERR_OOM, "no host memory");
+    }
+}
+
 #define HIP_TRY(ctx, expr)                                                                        \
     do {                                                                                          \
         hipError_t e__ = (expr);                                                                  \

@@ -178,17 +178,6 @@ static int relinearised_products(hisa_ctx* ctx, const ProductArgs& g, size_t ent
     });
 }
 
-// Nothing throws across the C boundary: what the host containers may throw (std::bad_alloc, std::length_error) becomes an error code.
-// The message needs no memory of its own: a std::string keeps 15 characters.
-template <class F>
-static int guarded(hisa_ctx* ctx, F body) {
-    try {
-        return body();
-    } catch (...) {
-        return fail(ctx, HISA_ERR_OOM, "no host memory");
-    }
-}
-
 // ---------------------------------------------------------------------------
 // gated linear recurrence
 // ---------------------------------------------------------------------------

@@ -124,3 +124,33 @@ assert before - free_memory() <= 8 << 20, before - free_memory()
 g.group_norm_plan_free(plan)
 g.close()
 ''')
+
+
+def test_any_allocation_of_a_key_may_fail(hook):
+    child(hook, r'''
+g = hisa.Context(13, [50] + [40] * 11, 3, 50, 7)
+g.keygen()
+g.gen_rot_mul_keys([3])
+ids = [0] + [k + g.galois_elt(3) for k in (0, 1 << 32)]
+keys = [g.key_export(k) for k in ids]
+made, taken = (hisa.Context(13, [50] + [40] * 11, 3, 50, 7) for _ in range(2))
+before = free_memory()
+n = 0
+while failing(n, made.gen_rot_mul_keys, [3])[0]:      # what one call made the next one keeps
+    n += 1
+assert n >= 6
+for k, key in zip(ids, keys):
+    for there in (False, True):
+        n = 0
+        while failing(n, taken.key_import, k, key)[0]:
+            n += 1
+        assert n > 0 or there
+for k, key in zip(ids, keys):
+    assert np.array_equal(taken.key_export(k), key) and (k == 0 or np.array_equal(made.key_export(k), key))
+# five keys, an export's scratch as large in each of two contexts, 2 MB for each to begin at and a few for their making.  The block and the
+# map's node are refused behind each of the five: ten more keys, if those were lost
+took, size = before - free_memory(), keys[0].nbytes
+assert size == 3 * 2 * 16 * 8192 * 8 and took <= 7 * (size + (2 << 20)) + (8 << 20), (took, size)
+for c in (g, made, taken):
+    c.close()
+''')
