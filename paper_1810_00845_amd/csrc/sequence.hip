@@ -80,7 +80,12 @@ static int need_fused(hisa_ctx* ctx, const char* what) {
     return HISA_OK;
 }
 
-static int check_scales(hisa_ctx* ctx, const hisa_tensor* t) {
+// A tensor that a layer takes: one scale, and no more elements to a ciphertext than it has slots (a stride of zero passes every
+// other check, whatever the extent, and masks and plans are encoded from host arrays of an entry an element).
+static int check_operand(hisa_ctx* ctx, const hisa_tensor* t) {
+    TRY(check_tensor(ctx, t));
+    if ((double)t_ci(t) * t->height * t->width > (double)(ctx->N / 2))
+        return fail(ctx, HISA_ERR_ARG, "%u x %u x %u elements do not fit %u slots", t_ci(t), t->height, t->width, ctx->N / 2);
     const double s = t->cts[0]->scale;
     if (!(s > 0.0) || !isfinite(s)) return fail(ctx, HISA_ERR_SCALE_MISMATCH, "a scale that is not a positive number");
     for (size_t i = 1; i < t_ncts(t); i++)
@@ -183,10 +188,8 @@ static int relinearised_products(hisa_ctx* ctx, const ProductArgs& g, size_t ent
 // ---------------------------------------------------------------------------
 // how many ciphertexts of x share a gate; both tensors have one layout
 static int check_gates(hisa_ctx* ctx, const hisa_tensor* gates, const hisa_tensor* x, unsigned* shared) {
-    TRY(check_tensor(ctx, gates));
-    TRY(check_tensor(ctx, x));
-    TRY(check_scales(ctx, gates));
-    TRY(check_scales(ctx, x));
+    TRY(check_operand(ctx, gates));
+    TRY(check_operand(ctx, x));
     if (gates->batch != x->batch || !same_slots(*gates, *x)) return fail(ctx, HISA_ERR_ARG, "gates and inputs have different layouts");
     if (x->channels % gates->channels || t_per(x) % t_per(gates) || x->channels / gates->channels != t_per(x) / t_per(gates))
         return fail(ctx, HISA_ERR_ARG, "%u channels do not share the gates of %u", x->channels, gates->channels);
@@ -416,8 +419,7 @@ extern "C" int hisa_recurrence_rot_steps(hisa_ctx* ctx, const hisa_tensor* like,
 
 // The gates of a row with zero at the token that has no predecessor: the masking multiply with that element left out
 static int recurrence_gates(hisa_ctx* ctx, const hisa_tensor* gates, bool reverse, const int64_t* coeffs, double scale, bool fixed, hisa_tensor* out) {
-    TRY(check_tensor(ctx, gates));
-    TRY(check_scales(ctx, gates));
+    TRY(check_operand(ctx, gates));
     if (!out || !out->cts || (fixed && (!coeffs || !(scale > 0.0)))) return fail(ctx, HISA_ERR_ARG, "bad argument");
     const uint32_t l = gates->cts[0]->limbs, ci = t_ci(gates), per = (uint32_t)t_per(gates), w = gates->width;
     if (l < 2) return fail(ctx, HISA_ERR_DEPTH_EXHAUSTED, "the masking multiply needs a level to rescale into");
@@ -609,8 +611,7 @@ static std::vector<std::vector<int32_t>> norm_sums(const hisa_ctx* ctx, const hi
 }
 
 static int check_norm(hisa_ctx* ctx, const hisa_tensor* t, const hisa_norm_geom* g) {
-    TRY(check_tensor(ctx, t));
-    TRY(check_scales(ctx, t));
+    TRY(check_operand(ctx, t));
     TRY(need_fused(ctx, "a normalisation"));
     TRY(check_clean(ctx, t, "inputs of a normalisation"));
     if (!g || g->groups == 0 || t->channels % g->groups || (g->groups > 1 && (t->channels / g->groups) % t_ci(t)))

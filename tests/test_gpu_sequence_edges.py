@@ -120,3 +120,28 @@ def test_a_plan_does_not_ask_for_strides_of_single_elements(shape, other):
         refused(ARG, g.group_norm_apply, t.shaped_like(w_stride=2, h_stride=8), plan)
     g.group_norm_plan_free(plan)
     g.close()
+
+
+def test_more_elements_than_slots_are_refused():
+    from paper_1810_00845_amd import hisa
+    g = hisa.Context(12, [50] + [BITS] * 6, 2, 50, 5)
+    t = g.tensor_encrypt(np.zeros((1, 2, 2, 3)), 2.0 ** BITS, 7)
+    g.keygen()
+    g.gen_rot_mul_keys(g.recurrence_rot_steps(t) + g.recurrence_rot_steps(t, False, True))
+    norm = (None, None, 1, 1e-3, 0.1, 4.0, 1)
+    plan = g.group_norm_prepare(t, *norm)
+    for many in (dict(h_stride=0, height=683), dict(h_stride=0, height=0xffffffff), dict(w_stride=0, h_stride=0, height=0xffffffff, width=0xffffffff),
+                 dict(w_stride=0, width=1025), dict(c_inner=0x80000000, c_stride=1, channels=0xffffffff)):
+        bad = t.shaped_like(**many)
+        refused(ARG, g.recurrence, bad, bad)
+        refused(ARG, g.recurrence_step, bad, bad, bad)
+        refused(ARG, g.recurrence_grad, bad, bad, bad)
+        refused(ARG, g.recurrence_gates, bad)
+        refused(ARG, g.group_norm_prepare_fixed, t.shaped_like(h_stride=0, height=683), np.zeros((2, g.N)), 2.0 ** 30, np.zeros((2, g.N)), *norm[2:])
+        refused(ARG, g.group_norm_apply, bad, plan)
+        if "channels" not in many:
+            refused(ARG, g.group_norm_prepare, bad, *norm)
+    full = t.shaped_like(h_stride=3, height=682)       # 2046 of 2048 slots
+    assert g.recurrence_gates(full).cts[0].limbs == 6
+    g.group_norm_plan_free(plan)
+    g.close()
