@@ -1988,6 +1988,23 @@ int relinearize_fp(hisa_ctx* ctx, const u64* cts3, size_t n, int l, u64* out) {
     return key_switch_core_fp(ctx, cts3 + 2 * lw, 3 * lw, 0, n, l, it->second, cts3, 3 * lw, 2, by, out);
 }
 
+int rotate_fp(hisa_ctx* ctx, const u64* in, u64 bs, size_t n, int l, int32_t steps, u64* out) {
+    if (!fused_key_switch_available(ctx)) return fail(ctx, HISA_ERR_ARG, "no fused key-switch path for these parameters");
+    const u64 g = galois_of(ctx, steps);
+    if (g == 0) return fail(ctx, HISA_ERR_ARG, "rotation by a multiple of the slot count");
+    if (t_analysis) {
+        t_analysis->steps.insert(norm_step(ctx, steps));
+        TALLY(rot_left, HISA_OP_ROT_LEFT, n, l);
+        TALLY(key_switch_calls, HISA_OP_KEY_SWITCH_CALLS, 1, l);
+        return HISA_OK;
+    }
+    auto it = ctx->keys.find(g);
+    if (it == ctx->keys.end()) return fail(ctx, HISA_ERR_NO_KEY, "no rotation key for %d slots (galois element %llu)", steps, (unsigned long long)g);
+    Division by;
+    TRY(division_by_p(ctx, l, false, &by));
+    return key_switch_core_fp(ctx, in + (u64)l * ctx->N, bs, g, n, l, it->second, in, bs, 1, by, out);
+}
+
 int product_keys_present(hisa_ctx* ctx, int32_t steps) {
     const u64 g = galois_of(ctx, steps);
     if (g == 0) return fail(ctx, HISA_ERR_ARG, "rotation by a multiple of the slot count");

@@ -323,6 +323,8 @@ struct CentreArgs {
 int centred_rescale_fp(hisa_ctx* ctx, const CentreArgs& g, size_t n, u64* out);      // divided by the last prime: out [n][2][limbs - 1][N]
 // three-polynomial ciphertexts -> two polynomials at the same level: [n][3][l][N] -> out [n][2][l][N]
 int relinearize_fp(hisa_ctx* ctx, const u64* cts3, size_t n, int l, u64* out);
+// ciphertexts [2][l][N], bs words apart, rotated by `steps` -> out [n][2][l][N]
+int rotate_fp(hisa_ctx* ctx, const u64* in, u64 bs, size_t n, int l, int32_t steps, u64* out);
 int rescale_fp(hisa_ctx* ctx, const u64* in, size_t n_polys, int l, u64* out);   // [n_polys][l][N] -> [n_polys][l - 1][N]
 
 // Optional per-kernel timing with HIP events on the launch stream (off by default; the benchmark

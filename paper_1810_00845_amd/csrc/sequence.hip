@@ -380,16 +380,19 @@ static int recurrence_grad(hisa_ctx* ctx, const hisa_tensor* gates, const hisa_t
     TRY(product_keys_present(ctx, back));
     const size_t n_x = t_ncts(grad), n_g = n_x / shared, n = ctx->N;
     const double sg = gates->cts[0]->scale, sx = grad->cts[0]->scale, sd = scan_scale(ctx, sg, sx, l, rounds);
-    std::vector<hisa_ct*> moved(n_g, nullptr);
-    TRY(hisa_rot_left_batch(ctx, (const hisa_ct* const*)gates->cts, n_g, on, moved.data()));
-    Outputs held(ctx);      // the moved gates, for the duration of the call
-    held.v = moved;
-    Gathered gh(ctx), gx(ctx);
+    Gathered gg(ctx), gh(ctx), gx(ctx);
+    TRY(gg.take(gates));
     TRY(gh.take(h));
     TRY(gx.take(grad));
+    const size_t words = ct_words(ctx, 2, (uint32_t)lg);
+    Temp moved(ctx, n_g * words * sizeof(u64));
+    if (!moved.ok()) return HISA_ERR_OOM;
+    TRY(in_parts(n_g, entries_at_once(ctx, lg, 1), [&](size_t e0, size_t cnt) {
+        return rotate_fp(ctx, gg.b.base + e0 * gg.b.stride, gg.b.stride, cnt, lg, on, moved.u() + e0 * words);
+    }));
     Outputs o(ctx), og(ctx);
     TRY(o.make(n_x, ld, sd));
-    TRY(scan_run(ctx, {moved[0]->data, ct_words(ctx, 2, (uint32_t)lg), lg}, sg, cts_of(gx.b, lx), n_x, shared, steps, l, o.data()));
+    TRY(scan_run(ctx, {moved.u(), words, lg}, sg, cts_of(gx.b, lx), n_x, shared, steps, l, o.data()));
     TRY(og.make(n_g, la - 1, sd * h->cts[0]->scale / (double)ctx->mod[la - 1]));
     ProductArgs g = product_base(ctx, la);
     g.n_first = (unsigned)n_g; g.terms = shared;

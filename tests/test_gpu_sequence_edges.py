@@ -145,3 +145,36 @@ def test_more_elements_than_slots_are_refused():
     assert g.recurrence_gates(full).cts[0].limbs == 6
     g.group_norm_plan_free(plan)
     g.close()
+
+
+# --- work in parts ---
+
+def launches(g, f):
+    """What f returned, and how often each kernel ran."""
+    g.profile_enable(True)
+    out = f()
+    counts = {k: n for k, (n, _ms) in g.profile_read().items()}
+    g.profile_enable(False)
+    return out, counts
+
+
+def row(g, cts, width):
+    from paper_1810_00845_amd import hisa
+    return hisa.CipherTensor(g, cts, 1, len(cts), 1, width, width, 1, 0, 1)
+
+
+def test_gates_of_a_gradient_are_moved_in_parts():
+    """130 gates, each with three digits of 22 limbs at N = 2^15: 17 MB, so 62 to a part of 1 GB."""
+    from paper_1810_00845_amd import hisa
+    g = hisa.Context(15, [50] + [BITS] * 15, 3, 50, 5)
+    n = 130
+    a, h, gr = (row(g, g.ct_random_batch(n, 16, 2.0 ** BITS, k), 2) for k in (1000, 2000, 3000))
+    g.gen_rot_mul_keys(g.recurrence_rot_steps(a, False, True))
+    (dx, dg), counts = launches(g, lambda: g.recurrence_grad(a, h, gr))
+    # the rows behind the columns of one polynomial's key switch: of the rotation alone
+    assert counts["ntt_fp_kernel<5, 6, false>"] == 3, counts
+    for i in (0, 43, 44, 86, 87, n - 1):      # around the parts' ends
+        few = g.recurrence_grad(*(row(g, t.cts[i:i + 1], 2) for t in (a, h, gr)))
+        for t, whole in zip(few, (dx, dg)):
+            assert np.array_equal(g.ct_export(t.cts[0]), g.ct_export(whole.cts[i]))
+    g.close()
