@@ -1,4 +1,6 @@
 """GPU: recurrences and group normalisation at the edges of what their layouts, plans and part sizes allow."""
+from dataclasses import replace
+
 import numpy as np
 import pytest
 
@@ -177,4 +179,145 @@ def test_gates_of_a_gradient_are_moved_in_parts():
         few = g.recurrence_grad(*(row(g, t.cts[i:i + 1], 2) for t in (a, h, gr)))
         for t, whole in zip(few, (dx, dg)):
             assert np.array_equal(g.ct_export(t.cts[0]), g.ct_export(whole.cts[i]))
+    g.close()
+
+
+PARTS = (15, [50] + [BITS] * 15, 3, 50, 5)      # an entry of a key switch at 16 limbs is 17 MB of digits, of a rotated product 35: 62 and 31 to a part
+
+
+def equal(g, one, many):
+    assert len(one) == len(many)
+    for a, b in zip(one, many):
+        assert np.array_equal(g.ct_export(a), g.ct_export(b))
+
+
+def test_scan_and_gradient_in_parts():
+    """141 ciphertexts, three to a gate: parts that begin inside a shared gate, hold the last tokens and the first gates, or gates alone; sums of
+    three products in parts.  Against every gate and its sharers alone, where a call is one part."""
+    from paper_1810_00845_amd import hisa
+    g = hisa.Context(*PARTS)
+    shared, n = 3, 141
+    a, x, h = (row(g, g.ct_random_batch(k, 16, 2.0 ** BITS, c), 3) for k, c in ((n // shared, 1000), (n, 2000), (n, 4000)))
+    g.gen_rot_mul_keys(g.recurrence_rot_steps(x) + g.recurrence_rot_steps(x, False, True))
+    out, counts = launches(g, lambda: g.recurrence(a, x))
+    # 188 entries at 16 limbs, 141 at 15 (32 to a part)
+    assert counts["product_rows_kernel<true>"] == 7 + 5, counts
+    (dx, dg), counts = launches(g, lambda: g.recurrence_grad(a, h, x))
+    assert counts["product_rows_kernel<true>"] == 7 + 5 + 2, counts         # 47 sums at 14 limbs, 34 to a part
+    for i in (0, 8, 9, 10, 23, 24, 36, n // shared - 1):
+        own = slice(i * shared, (i + 1) * shared)
+        ai, xi, hi = row(g, a.cts[i:i + 1], 3), row(g, x.cts[own], 3), row(g, h.cts[own], 3)
+        equal(g, g.recurrence(ai, xi).cts, out.cts[own])
+        one = g.recurrence_grad(ai, hi, xi)
+        equal(g, one[0].cts, dx.cts[own])
+        equal(g, one[1].cts, dg.cts[i:i + 1])
+    # as many gates as inputs: the second of two parts begins with the first gate
+    a, x = row(g, x.cts[:31], 3), row(g, x.cts[31:62], 3)
+    out, counts = launches(g, lambda: g.recurrence(a, x))
+    assert counts["product_rows_kernel<true>"] == 2 + 1, counts
+    for i in range(0, 31, 6):
+        equal(g, g.recurrence(row(g, a.cts[i:i + 1], 3), row(g, x.cts[i:i + 1], 3)).cts, out.cts[i:i + 1])
+    g.close()
+
+
+def test_single_tokens_in_parts():
+    from paper_1810_00845_amd import hisa
+    g = hisa.Context(*PARTS)
+    g.keygen()
+    shared, n = 3, 141
+    a, s, x = (row(g, g.ct_random_batch(k, 16, 2.0 ** BITS, c), 2) for k, c in ((n // shared, 1000), (n, 2000), (n, 4000)))
+    out, counts = launches(g, lambda: g.recurrence_step(a, s, x))
+    assert counts["product_rows_kernel<false>"] == 3, counts        # 47 each: the second begins with the last sharer of a gate
+    for i in (0, 15, 16, 31, 32, n // shared - 1):
+        own = slice(i * shared, (i + 1) * shared)
+        equal(g, g.recurrence_step(row(g, a.cts[i:i + 1], 2), row(g, s.cts[own], 2), row(g, x.cts[own], 2)).cts, out.cts[own])
+    g.close()
+
+
+@pytest.mark.parametrize("groups,products", [(9, 1 + 1 + 1 + 2 + 2), (45, 3 + 4 + 2 + 2 + 2)])
+def test_normalisation_in_parts(groups, products):
+    """Three images of 45 channels: groups of five, whose products with one 1 / sqrt are in two parts that begin inside a group and an image,
+    and of one, where relinearisations, sums of rotations and the products of the variances are in parts too.  Against every group alone."""
+    from paper_1810_00845_amd import hisa
+    g = hisa.Context(*PARTS)
+    g.keygen()
+    batch, channels = 3, 45
+    per = channels // groups
+    cts = g.ct_random_batch(batch * channels, 16, 2.0 ** BITS, 1000)
+    t = hisa.CipherTensor(g, cts, batch, channels, 1, 3, 3 * 512, 512, 0, 1)       # five doublings: two sums
+    g.gen_rot_keys(g.group_norm_rot_steps(t))
+    rng = np.random.default_rng(groups)
+    gamma, beta = rng.uniform(0.5, 1.5, channels), rng.uniform(-1, 1, channels)
+    args = (1e-3, 0.1, 1.0, 1)
+    plan = g.group_norm_prepare(t, gamma, beta, groups, *args, act_ratio=0.5)
+    y, counts = launches(g, lambda: g.group_norm_apply(t, plan))
+    # the variances at 16 limbs, an iteration's pair at 14 and product at 13, the normalised values at 12, their activation at 11.  A digit has
+    # limbs + 6 limbs of 256 KB, three digits down to 13 limbs, then two: 62, 68, 71, 113 and 120 entries to a part of 1 GB
+    assert counts["product_rows_kernel<false>"] == products, counts
+    g.group_norm_plan_free(plan)
+    for e in (0, 67, 68, 90, 134):
+        b, first = e // channels, e % channels // per * per
+        own = slice(b * channels + first, b * channels + first + per)
+        one = hisa.CipherTensor(g, cts[own], 1, per, 1, 3, 3 * 512, 512, 0, 1)
+        plan = g.group_norm_prepare(one, gamma[first:first + per], beta[first:first + per], 1, *args, act_ratio=0.5)
+        equal(g, g.group_norm_apply(one, plan).cts, y.cts[own])
+        g.group_norm_plan_free(plan)
+    g.close()
+
+
+# --- kernels that only larger calls and other parameters reach ---
+
+def test_chains_of_sums_by_rows_of_one_wave():
+    """Sixteen groups at 9 limbs, N = 2^12: the rows between two sums are 2304, more than four waves a row serve.  Bits against the oracle and
+    against a group alone."""
+    from oracle import sequence as seq
+    from paper_1810_00845_amd import synth
+    g, o = pair(12, 9, 3)
+    gt, ot = random_tensors(g, o, 16, 9, 2.0 ** BITS, 3, batch=16, height=1, width=3, w_stride=64)
+    steps = g.group_norm_rot_steps(gt)
+    g.gen_rot_keys(steps); o.gen_rot_keys(steps)
+    gamma, beta = (np.stack([synth.plaintext_coeffs(k, g.N, bits)]) for k, bits in ((7, 30), (70, 40)))
+    args = (1, 1e-3, 0.05, 2.0, 1)
+    plan = g.group_norm_prepare_fixed(gt, gamma, 2.0 ** 35, beta, *args)
+    y, counts = launches(g, lambda: g.group_norm_apply(gt, plan))
+    assert counts["final_inverse_rows_kernel"] == 1 and "final_inverse_wide_kernel" not in counts, counts
+    for i in range(16):
+        one, counts = launches(g, lambda: g.group_norm_apply(gt.shaped_like(cts=gt.cts[i:i + 1], batch=1), plan))
+        assert counts["final_inverse_wide_kernel"] == 1
+        equal(g, one.cts, y.cts[i:i + 1])
+    for i in (0, 15):
+        want = seq.group_norm_fixed(o, replace(ot, cts=ot.cts[i:i + 1], batch=1), gamma, 2.0 ** 35, beta, *args)
+        assert np.array_equal(g.ct_export(y.cts[i]), o.export(want.cts[0]))
+    g.group_norm_plan_free(plan)
+    g.close()
+
+
+@pytest.mark.parametrize("limbs,dnum,gates,x", [(9, 8, 2, 6), (8, 8, 5, 5), (10, 5, 1, 4)])
+def test_pairs_of_more_than_four_digits(limbs, dnum, gates, x):
+    """Inner products of four pairs at a time, the last ones part filled."""
+    from oracle import sequence as seq
+    g, o = pair(12, limbs, dnum)
+    ga, oa = random_tensors(g, o, gates, limbs, 2.0 ** BITS, 1, width=3)
+    gx, ox = random_tensors(g, o, x, limbs, 2.0 ** BITS, 2, width=3)
+    steps = g.recurrence_rot_steps(gx)
+    g.gen_rot_mul_keys(steps); seq.gen_rot_mul_keys(o, steps)
+    out, counts = launches(g, lambda: g.recurrence(ga, gx))
+    assert counts["pair_inner_kernel"] >= 1, counts
+    same(g, o, out, seq.recurrence(o, oa, ox))
+    g.close()
+
+
+def test_dry_run_of_a_gradient():
+    from paper_1810_00845_amd import hisa
+    g = hisa.Context(12, [50] + [BITS] * 7, 2, 50, 5)
+    like = g.tensor_encrypt(np.zeros((1, 4, 1, 6)), 2.0 ** BITS, 8)
+    g.analysis_begin()
+    x, h = (g.tensor_encrypt(np.zeros((1, 4, 1, 6)), 2.0 ** BITS, 8) for _ in range(2))
+    a = g.tensor_encrypt(np.zeros((1, 2, 1, 6)), 2.0 ** BITS, 8)
+    dx, dg = g.recurrence_grad(a, h, x, True)
+    counts, steps = g.analysis_end()
+    assert sorted(steps) == sorted(g.recurrence_rot_steps(like, True, True))
+    assert (len(dx.cts), dx.cts[0].limbs, len(dg.cts), dg.cts[0].limbs) == (4, 5, 2, 4) and counts["min_limbs"] == 4
+    # the gates moved, three rounds on four ciphertexts and (but for the last) two gates, two sums of products
+    assert counts["rot_left"] == 2 + 3 * 4 + 2 * 2 + 2 and counts["relinearize"] == counts["mul"] == 3 * 4 + 2 * 2 + 2
     g.close()
