@@ -254,6 +254,7 @@ int moddown_add_fp(hisa_ctx* ctx, const u64* acc, size_t B, int l, const u64* ad
 u64 double_to_residue(double v, u64 q);
 
 // ---- tensors (layers.hip), shared with the sequence layers (sequence.hip) ----
+// channels per ciphertext (0 in a zero-initialised struct means HW-tiling), ciphertexts per image, ciphertexts in all
 static inline uint32_t t_ci(const hisa_tensor* t) { return t->c_inner ? t->c_inner : 1; }
 static inline size_t t_per(const hisa_tensor* t) { return ((size_t)t->channels + t_ci(t) - 1) / t_ci(t); }
 static inline size_t t_ncts(const hisa_tensor* t) { return (size_t)t->batch * t_per(t); }

@@ -1047,7 +1047,6 @@ static hipError_t launch_plain_mac(hisa_ctx* ctx, const PrimeConst* primes, cons
 // ---------------------------------------------------------------------------
 // helpers
 // ---------------------------------------------------------------------------
-// channels per ciphertext (0 in a zero-initialised struct means HW-tiling), ciphertexts per image, ciphertexts in all
 static int check_layout(hisa_ctx* ctx, const hisa_tensor* t) {
     if (!t || !t->cts || t->batch == 0 || t->channels == 0 || t->height == 0 || t->width == 0)
         return fail(ctx, HISA_ERR_ARG, "empty tensor");

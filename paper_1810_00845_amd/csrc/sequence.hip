@@ -537,7 +537,6 @@ struct NormSchedule {
     struct Step { double y, product; };
     std::vector<Step> steps;     // an iteration: y <- (y's factor) y - (the product's) (w y) (y y)
     int level_y;                 // of 1 / sqrt
-    double sum_scale;            // of (x - mean) gamma / gamma_scale before the division by q
     double scale_y;
     int out_level;
     double norm_scale, act, out_scale;
