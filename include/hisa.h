@@ -546,7 +546,8 @@ int hisa_avg_pool2x2(hisa_ctx* ctx, const hisa_tensor* in, hisa_tensor* out);
 int hisa_poly2_act(hisa_ctx* ctx, const hisa_tensor* in, double a, double b, hisa_tensor* out);
 /* ---- layers of sequence models (no counterpart in the paper; its interface is what they are made of) ----
  * They need what hisa_rot_left_sum_batch needs (HISA_ERR_ARG otherwise), clean tensors, and one scale per tensor
- * (HISA_ERR_SCALE_MISMATCH).  Operands may differ in level: each is used at the lowest one among them.
+ * (HISA_ERR_SCALE_MISMATCH).  Operands may differ in level: each is used at the lowest one among them.  A tensor has at most 16384
+ * ciphertexts, and no more elements to a ciphertext than slots (HISA_ERR_ARG).
  *
  * Gated linear recurrence along the width of a tensor, every row (batch, channel, y) a sequence of its own:
  *     h[t] = x[t] + gates[t] h[t - 1],  h[first] = x[first];  reverse != 0: h[t] = x[t] + gates[t] h[t + 1]

@@ -1660,6 +1660,8 @@ static hipError_t launch_step_rows_once(int mode, dim3 grid, const ConvertArgs& 
 // Digit d of the 2 half that a.n_digits counts (at most FP_MAX_DIGITS) is digit d / 2 of the first polynomial or, d odd, of the second:
 // of the two waves of a task each has a polynomial's digits, and the round of a limb's own digits, which need no transform, is the same
 // for both.  The first polynomial's digits in front of the second's have one wave wait for the other in two rounds of three.
+// Fifteen pairs at N = 2^15, 16 limbs, three digits: the limbs of q 189 us, bound by memory (0.76 GB counted, 4.0 TB/s of a copy's 4.6; issue at 0.58
+// of the rate of additions); the special limbs 94 us, by neither alone (0.26 GB, 2.7 TB/s; 0.61).
 template <int K3, int MODE>
 __global__ __launch_bounds__(128, 4) void inner_product_pair_rows_kernel(ConvertArgs a, InnerArgs g, PairArgs s, int n_tasks) {
     __shared__ double lds[2 * ROW_LDS];
@@ -1717,8 +1719,8 @@ hipError_t launch_inner_pair_rows_fp(int mode, const ConvertArgs& a, const Inner
 // A workgroup per (limb, row, entry), four waves per polynomial: with b rotated, waves of polynomial u form a_u sigma(b0) + f c_u, which
 // needs no key, and a_u sigma(b1), whose inverse rows they go on with; else the first four form the two polynomials of the result and
 // the others a1 b1 and its inverse rows.
-// Bound by memory (4.4 TB/s of what it cannot do without at 38 products, N = 2^15, 16 limbs), by its chain of loads, products and ten
-// levels where it is small.  As two launches / here: those 38 products 299 / 295 us, one at N = 2^13, 8 limbs 8.0 / 6.5, two rotated at
+// Bound by memory (4.4 TB/s of what it cannot do without at 38 products, N = 2^15, 16 limbs; 15 rotated ones 129 us, 0.62 GB counted, 4.8 TB/s), by its
+// chain of loads, products and ten levels where it is small.  As two launches / here: those 38 products 299 / 295 us, one at N = 2^13, 8 limbs 8.0 / 6.5, two rotated at
 // N = 2^15, 21 limbs 20.1 / 16.
 // Ranges: factors canonical, products within 0.875 p, at most four more on a normalised value.
 #define PRODUCT_NT (2 * WIDE_NT)

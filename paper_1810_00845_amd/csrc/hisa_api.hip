@@ -1912,7 +1912,9 @@ static bool store_accumulators(const hisa_ctx* ctx, size_t entries, int ext_limb
 
 // Of pairs: six digits are a longer chain of rounds, and memory stays ahead up to twice as many rows.  Scan of 100 tokens at N = 2^14, 12 limbs,
 // three ciphertexts (1024 rows, 960, ..) 679 -> 633 us, of 16384 at N = 2^15, 21 limbs (1792, 1728, ..) 1571 -> 1493; of twelve ciphertexts
-// there, 16 limbs (10560 ..) 2538 / 2547, four and two of 21 limbs (5376 ..) 2885 / 2891.
+// there, 16 limbs (10560 ..) 2538 / 2547, four and two of 21 limbs (5376 ..) 2885 / 2891.  Around the line, one round, in registers / in memory:
+// N = 2^14, 12 limbs 1024 rows 97 / 86, 1536 117 / 113, 2048 141 / 136, 2560 181 / 181, 4096 243 / 250; N = 2^15, 12 limbs 1728 115 / 116, 2304
+// 130 / 136, 3456 187 / 195; 16 limbs 2112 160 / 160, 2816 189 / 194, 4224 274 / 278; 21 limbs 1792 158 / 154, 2688 204 / 209, 4480 297 / 305.
 static bool store_pair_accumulators(const hisa_ctx* ctx, size_t entries, int ext_limbs) {
     return entries * (size_t)ext_limbs * (ctx->N >> 10) < 2048;
 }

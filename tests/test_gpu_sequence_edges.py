@@ -143,6 +143,11 @@ def test_more_elements_than_slots_are_refused():
         refused(ARG, g.group_norm_apply, bad, plan)
         if "channels" not in many:
             refused(ARG, g.group_norm_prepare, bad, *norm)
+    crowd = t.shaped_like(cts=t.cts[:1] * 16385, channels=16385)
+    refused(ARG, g.recurrence, crowd, crowd)
+    refused(ARG, g.recurrence_step, crowd, crowd, crowd)
+    refused(ARG, g.recurrence_grad, crowd, crowd, crowd)
+    refused(ARG, g.group_norm_prepare, crowd, *norm)
     full = t.shaped_like(h_stride=3, height=682)       # 2046 of 2048 slots
     assert g.recurrence_gates(full).cts[0].limbs == 6
     g.group_norm_plan_free(plan)
