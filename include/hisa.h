@@ -42,7 +42,7 @@ extern "C" {
 #define HISA_ERR_NO_KEY (-4)          /* rotation amount / relin without a generated key */
 #define HISA_ERR_BAD_DIVISOR (-5)     /* divScalar with x != maxScalarDiv(c, ub)         */
 #define HISA_ERR_DEPTH_EXHAUSTED (-6) /* rescale of a one-limb ciphertext                */
-#define HISA_ERR_OOM (-7)             /* device allocation failed                        */
+#define HISA_ERR_OOM (-7)             /* device or host allocation failed                */
 #define HISA_ERR_HIP (-8)             /* a HIP runtime call or kernel launch failed      */
 #define HISA_ERR_SIZE (-9)            /* wrong number of polynomials for this operation  */
 
