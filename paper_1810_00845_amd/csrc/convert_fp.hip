@@ -1719,9 +1719,9 @@ hipError_t launch_inner_pair_rows_fp(int mode, const ConvertArgs& a, const Inner
 // A workgroup per (limb, row, entry), four waves per polynomial: with b rotated, waves of polynomial u form a_u sigma(b0) + f c_u, which
 // needs no key, and a_u sigma(b1), whose inverse rows they go on with; else the first four form the two polynomials of the result and
 // the others a1 b1 and its inverse rows.
-// Bound by memory (4.4 TB/s of what it cannot do without at 38 products, N = 2^15, 16 limbs; 15 rotated ones 129 us, 0.62 GB counted, 4.8 TB/s), by its
-// chain of loads, products and ten levels where it is small.  As two launches / here: those 38 products 299 / 295 us, one at N = 2^13, 8 limbs 8.0 / 6.5, two rotated at
-// N = 2^15, 21 limbs 20.1 / 16.
+// Bound by memory (4.4 TB/s of what it cannot do without at 38 products, N = 2^15, 16 limbs; 15 rotated ones 129 us, 0.62 GB counted,
+// 4.8 TB/s), by its chain of loads, products and ten levels where it is small.  As two launches / here: those 38 products 299 / 295 us, one at
+// N = 2^13, 8 limbs 8.0 / 6.5, two rotated at N = 2^15, 21 limbs 20.1 / 16.
 // Ranges: factors canonical, products within 0.875 p, at most four more on a normalised value.
 #define PRODUCT_NT (2 * WIDE_NT)
 template <int K3, bool ROTATED>

@@ -587,8 +587,8 @@ __device__ __forceinline__ void key_load2(rsrc_t r, uint32_t lane_off, uint32_t 
 // 346), of twelve 531, 721, 1130 / 524, 645, 910; at N = 2^14, 12 limbs eight 116, 151, 229 / 113, 134, 188; of two 139, 180, 268 / 136, 185,
 // 268 and of one 134 / 150 (seven): those stay above.  A missing output of a last group is computed for nothing: the kernel alone, of 3, 5, 6, 9
 // and 13 outputs at N = 2^15, 16 limbs, three rotations 53, 76, 86, 126, 174 / 49, 79, 86, 123, 182, seven 96, 151, 168, 236, 326 / 86, 134, 144,
-// 208, 300, 15 183, 316, 352, 508, 704 / 155, 250, 266, 380, 576; one rotation the same within 1 us.  Only three rotations of one output more
-// than full groups lose, 4 % here and 1 % of the whole sum.
+// 208, 300, 15 183, 316, 352, 508, 704 / 155, 250, 266, 380, 576; one rotation the same within 1 us.  Only three rotations of 5 and of 13
+// lose, 4 and 5 %, which is 1 % of the whole sum.
 #define HALVES_NT 256
 static hipError_t launch_sum_halves(const SumArgs& g, int digits, bool once, hipStream_t st);
 template <int DIGITS, bool ONCE>
